@@ -325,6 +325,71 @@ int ee_ir_set(ee_ctx* ctx, int layer, const int* cfg, int n);
 int ee_group_table(const ee_ctx* ctx, int layer, int* cfg_out, int n);
 int ee_group_set(ee_ctx* ctx, int layer, const int* cfg, int n);
 
+/* ---- operators on a batch of in-flight requests, outside a network -------------------------------------------------------
+ * Calls of their own: they need no ctx.  Device work goes to `hip_stream` (a stream of the current device) and is asynchronous; nothing
+ * is allocated: what a call needs beyond its outputs it takes from `workspace`, device memory of at least the size its _workspace call
+ * names (256-byte aligned; it may be NULL where that is 0), which must be the call's own until it has run: two calls that may overlap,
+ * replays of captured graphs included, need a workspace each.  Strides are in elements.  The calls may be captured into a graph. */
+
+enum { EE_ACT_NONE = 0, EE_ACT_RELU = 1, EE_ACT_RELU6 = 2, EE_ACT_SILU = 3 };
+
+/* Group norm with an activation, channels last.  x[b][pixels][c] (int8 or bf16), channels are neighbours, sample and pixel strides are free: a channel slice of a wider tensor is one.
+ * Group g of a sample is channels [g c / groups, (g + 1) c / groups) of all its pixels, n values; var is their variance (divided by n).
+ *   bf16  y = act(weight (x - mean) / sqrt(var + eps) + bias + res), computed in float and rounded once; a NaN in a group makes the group NaN
+ *   int8  y = clamp(floor(d m + (bias 2^frac_bits + 1/2) + res 2^res_shift), lo, hi) with d = n x - sum x (exact) and
+ *         m = weight 2^frac_bits / (n sqrt(var + eps)), in 64-bit floats; [lo, hi] = [-128, 127], with RELU [0, 127], with RELU6 [0, min(127, 6 * 2^frac_bits)]
+ * weight, bias   device float[c], or NULL (1, 0);  res   device, the shape and type of x, added in front of the activation, or NULL
+ * y may be x or res with its strides; otherwise it must not overlap them.  b == 0 or pixels == 0 is a no-op.
+ * EE_ERR_ARG: c not a multiple of groups, eps < 0 or not finite, frac_bits outside 0..7, res_shift outside -8..8, unknown act;  EE_ERR_UNSUPPORTED: SILU with int8, a group of more than
+ * 1024 channels (8192 in bf16, 16384 in int8 where they are whole 16-byte pieces and x, y, res and their strides are 16-byte aligned);  EE_ERR_OVERFLOW: int8 groups of 2^24 values or more, 2^31 pixels x channels of a sample or more, too small a workspace. */
+typedef struct {
+    int32_t dtype, act, b, pixels, c, groups, frac_bits, res_shift;
+    float eps; int32_t pad_;
+    int64_t x_sample, x_pixel, res_sample, res_pixel, y_sample, y_pixel;
+} ee_norm_desc;
+int ee_group_norm_workspace(const ee_norm_desc* desc, int64_t* bytes);
+int ee_group_norm(const ee_norm_desc* desc, const void* x, const float* weight, const float* bias, const void* res, void* y,
+                  void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* A shared projection with each request's low-rank adapter beside it (bf16): for every row m of x, with a the adapter of its slot,
+ *   y[m][o] = sum_c x[m][c] w[o][c] + bias[o] + scale_a sum_r b_a[o][r] (sum_c a_a[r][c] x[m][c])
+ * Sums are in float; the inner one is rounded to 2^-18 relative for bf16 results, to 2^-24 for float ones.  y is bf16 or float.
+ * Weights are laid out once: ee_adapter_bytes sizes the two device buffers (256-byte aligned) a program keeps, ee_adapter_pack fills the first with w[co][ci] and bias (float[co] or
+ * NULL), ee_adapter_load puts adapter i (a[rank][ci], b[co][rank], rank <= dims->rank) into the second, also between calls; rank 0 takes it out again (a, b may be NULL).  The second buffer
+ * must be zero before its first use (then no adapter adds anything).
+ * A call: `rows` rows, `ldx` / `ldy` apart, belong to `slots` slots: `per` rows each (rows = slots * per), or, with offsets (device int32[slots + 1], not decreasing, per is not used), rows
+ * [offsets[s], offsets[s + 1]) to slot s; rows in front of offsets[0] or from offsets[slots] on belong to none: they are left as they were in y, and what x holds there does not matter.
+ * ids: device int32[slots], the slot's adapter; outside [0, adapters): none.  It may be NULL when adapters = 0.
+ * EE_ERR_ARG: NULL or misaligned pointers, rows != slots * per, ldx < ci, ldy < co;  EE_ERR_OVERFLOW: ci or co above 2^18, rank above 256, adapters above 65536, rows above 2^22, too small a workspace. */
+typedef struct { int32_t ci, co, adapters, rank; } ee_adapter_dims;
+typedef struct {
+    const void* packed; const void* pool; const void* x; void* y; const int32_t* ids; const int32_t* offsets;
+    int64_t ldx, ldy; int32_t rows, slots, per, out_f32;
+    void* workspace; int64_t workspace_bytes;
+} ee_adapter_call;
+int ee_adapter_bytes(const ee_adapter_dims* dims, int64_t* packed_bytes, int64_t* pool_bytes);
+int ee_adapter_pack(const ee_adapter_dims* dims, const void* w, int64_t ldw, const float* bias, void* packed, void* hip_stream);
+int ee_adapter_load(const ee_adapter_dims* dims, int i, int rank, const void* a, int64_t lda, const void* b, int64_t ldb, float scale, void* pool, void* hip_stream);
+int ee_adapter_workspace(const ee_adapter_dims* dims, int rows, int64_t* bytes);
+int ee_adapter_project(const ee_adapter_dims* dims, const ee_adapter_call* call, void* hip_stream);
+
+/* Verification of drafted tokens (an early exit drafts, the last one verifies) against the target's probabilities p[b][k + 1][v], from given random numbers u[b][k + 1].
+ * Per sequence: draft i of draft[b][k] is accepted while u_i q_i(x_i) < p_i(x_i), with q[b][k][v] the probabilities it was drawn from, or NULL: it was certain (q = 1 at it, 0 elsewhere);
+ * a draft outside [0, v) is refused.  Then one token more is drawn: behind a refusal at n from weights max(p_n - q_n, 0) (from p_n where these are all zero), where all were accepted from
+ * p_n: the first j with w_0 + .. + w_j > u_k sum(w), or the last of positive weight.  Weights that are not finite and positive count as 0; if all are, the token is -1.
+ *   lengths        device int32[b], or NULL: drafts of the sequence, at most k count; < 0: an empty slot (nothing accepted, all tokens -1)
+ *   accepted[b]    device int32: drafts accepted;  tokens[b][k + 1] device int32: the accepted drafts, the drawn token, -1 behind it
+ * p and q are float or bf16 (f32 = 1 or 0), entries of a row are neighbours.  The products and sums are in 64-bit floats, added in one order whatever else runs.  b == 0 is a no-op, k may be 0.
+ * EE_ERR_ARG: NULL pointers, v < 1, b or k < 0;  EE_ERR_OVERFLOW: v above 2^30, b (k + 1) above 2^28, b of 2^23 or more, too small a workspace. */
+typedef struct {
+    const int32_t* draft; const void* p; const void* q; const float* u; const int32_t* lengths; int32_t* accepted; int32_t* tokens;
+    int64_t draft_row, u_row, p_seq, p_row, q_seq, q_row;
+    int32_t b, k, v, f32;
+    void* workspace; int64_t workspace_bytes;
+} ee_verify_call;
+int ee_verify_workspace(int b, int k, int v, int64_t* bytes);
+int ee_verify_draft(const ee_verify_call* call, void* hip_stream);
+
 /* Host copy of the 256-entry table round(2^30 * 2^(-i/256)) used by the integer softmax. */
 const uint32_t* ee_exp2_table(void);
 

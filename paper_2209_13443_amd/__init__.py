@@ -26,7 +26,9 @@ SYMBOLS = ["ee_strerror", "ee_blob_check", "ee_create", "ee_destroy", "ee_query"
            "ee_compact_refill", "ee_serve_stream", "ee_schedule_sim", "ee_measure_lut", "ee_profile_enable",
            "ee_profile_read", "ee_kernel_name", "ee_exp2_table", "ee_tune_conv_tile", "ee_ir_count", "ee_ir_layers", "ee_ir_mode", "ee_ir_table", "ee_ir_set", "ee_group_table", "ee_group_set", "ee_last_logits", "ee_profile_reserve", "ee_autotune", "ee_config_table",
            "ee_pair_count", "ee_pair_mode", "ee_pair_table", "ee_config_set", "ee_pair_set", "ee_exit_head_static",
-           "ee_static_scratch_bytes", "ee_time_layer", "ee_lanes", "ee_zero_copy_supported"]
+           "ee_static_scratch_bytes", "ee_time_layer", "ee_lanes", "ee_zero_copy_supported", "ee_group_norm_workspace", "ee_group_norm",
+           "ee_adapter_bytes", "ee_adapter_pack", "ee_adapter_load", "ee_adapter_workspace", "ee_adapter_project", "ee_verify_workspace", "ee_verify_draft"]
+ACTS = {"none": 0, "relu": 1, "relu6": 2, "silu": 3}
 
 
 class Trace(C.Structure):
@@ -46,6 +48,26 @@ class ServeStats(C.Structure):
 
 class KernelStat(C.Structure):
     _fields_ = [("launches", C.c_int64), ("ms", C.c_double), ("ops", C.c_double), ("bytes", C.c_double)]
+
+
+class NormDesc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "act", "b", "pixels", "c", "groups", "frac_bits", "res_shift")] + [("eps", C.c_float), ("pad_", C.c_int32)] +
+                [(n, C.c_int64) for n in ("x_sample", "x_pixel", "res_sample", "res_pixel", "y_sample", "y_pixel")])
+
+
+class AdapterDims(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("ci", "co", "adapters", "rank")]
+
+
+class AdapterCall(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("packed", "pool", "x", "y", "ids", "offsets")] + [("ldx", C.c_int64), ("ldy", C.c_int64)] +
+                [(n, C.c_int32) for n in ("rows", "slots", "per", "out_f32")] + [("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)])
+
+
+class VerifyCall(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("draft", "p", "q", "u", "lengths", "accepted", "tokens")] +
+                [(n, C.c_int64) for n in ("draft_row", "u_row", "p_seq", "p_row", "q_seq", "q_row")] +
+                [(n, C.c_int32) for n in ("b", "k", "v", "f32")] + [("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)])
 
 
 if not os.path.exists(LIB_PATH):
@@ -89,6 +111,15 @@ _lib.ee_group_set.argtypes = [_V, C.c_int, _V, C.c_int]
 _lib.ee_profile_enable.argtypes = [_V, C.c_int]
 _lib.ee_profile_read.argtypes = [_V, _V, _V]
 _lib.ee_profile_reserve.argtypes = [_V, C.c_int64]
+_lib.ee_group_norm_workspace.argtypes = [_V, _V]
+_lib.ee_group_norm.argtypes = [_V] * 7 + [C.c_int64, _V]
+_lib.ee_adapter_bytes.argtypes = [_V, _V, _V]
+_lib.ee_adapter_pack.argtypes = [_V, _V, C.c_int64, _V, _V, _V]
+_lib.ee_adapter_load.argtypes = [_V, C.c_int, C.c_int, _V, C.c_int64, _V, C.c_int64, C.c_float, _V, _V]
+_lib.ee_adapter_workspace.argtypes = [_V, C.c_int, _V]
+_lib.ee_adapter_project.argtypes = [_V, _V, _V]
+_lib.ee_verify_workspace.argtypes = [C.c_int, C.c_int, C.c_int, _V]
+_lib.ee_verify_draft.argtypes = [_V, _V]
 
 
 class EEError(RuntimeError):
@@ -358,3 +389,189 @@ class Engine:
         if not n_layers:
             return cls
         return cls, [dict(launches=x.launches, ms=x.ms, ops=x.ops, bytes=x.bytes) for x in lay]
+
+
+# -- operators on a batch of in-flight requests, outside a network: on the current stream of their tensors' device --------------
+def _need(ok, what, code=EE_ERR_ARG):
+    if not ok:
+        e = EEError(code)
+        e.args = (f"{e.args[0]}: {what}",)
+        raise e
+
+
+def _on(device, f):
+    """f(stream handle) with `device` current."""
+    if device.index == torch.cuda.current_device():
+        return f(torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(device):
+        return f(torch.cuda.current_stream().cuda_stream)
+
+
+def _tensor(t, name, dtypes, device):
+    _need(isinstance(t, torch.Tensor) and t.dtype in dtypes, f"{name} has to be a tensor of {' or '.join(str(d) for d in dtypes)}", EE_ERR_UNSUPPORTED)
+    _need(t.device == device and device.type == "cuda", f"{name} has to be on the GPU, all tensors on the same one")
+
+
+def _pixels(t, name):
+    """(samples, pixels, channels, sample stride, pixel stride) of [b, ..., c]; the dimensions between have to lie behind one another."""
+    _need(t.dim() >= 2 and (t.shape[-1] == 1 or t.stride(-1) == 1), f"{name} has to be [samples, ..., channels] with neighbouring channels")
+    pixels, step = 1, 0
+    for n, s in zip(t.shape[-2:0:-1], t.stride()[-2:0:-1]):
+        if n > 1:
+            _need(step == 0 or s == step * pixels, f"the pixels of {name} have to lie one stride apart")
+            step = step or s
+        pixels *= n
+    return t.shape[0], pixels, t.shape[-1], t.stride(0), step or t.shape[-1]
+
+
+def _workspace(bytes_, device):
+    return torch.empty(bytes_, dtype=torch.uint8, device=device) if bytes_ else None
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def group_norm(x, groups, weight=None, bias=None, eps=1e-5, act="none", residual=None, frac_bits=0, res_shift=0, out=None):
+    """ee_group_norm: act(group norm of x + residual) on x[b, ..., c] (int8, bfloat16 or int16 holding bf16 bits; any sample stride, one pixel stride, channel slices included).
+    weight, bias: float32 [c].  act: "none", "relu", "relu6", "silu" (not int8).  int8: the result is in units of 2^-frac_bits, the residual enters times 2^res_shift."""
+    dev = x.device
+    _tensor(x, "x", (torch.bfloat16, torch.int8, torch.int16), dev)
+    b, pixels, c, sample, pixel = _pixels(x, "x")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        y = (b, pixels, c, pixels * c, c)
+    else:
+        _tensor(out, "out", (x.dtype,), dev)
+        y = _pixels(out, "out")
+    _need(out.shape == x.shape, "out has to have the shape of x")
+    r = (0, 0, 0, 0, 0)
+    if residual is not None:
+        _tensor(residual, "residual", (x.dtype,), dev)
+        _need(residual.shape == x.shape, "residual has to have the shape of x")
+        r = _pixels(residual, "residual")
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is not None:
+            _tensor(t, name, (torch.float32,), dev)
+            _need(t.shape == (c,) and t.is_contiguous(), f"{name} has to be dense [channels]")
+    _need(act in ACTS, f"act has to be one of {', '.join(ACTS)}")
+    d = NormDesc(EE_I8 if x.dtype == torch.int8 else EE_BF16, ACTS[act], b, pixels, c, groups, frac_bits, res_shift, eps, 0, sample, pixel, r[3], r[4], y[3], y[4])
+    need = C.c_int64()
+    _chk(_lib.ee_group_norm_workspace(C.byref(d), C.byref(need)))
+
+    def call(stream):
+        ws = _workspace(need.value, dev)
+        _chk(_lib.ee_group_norm(C.byref(d), x.data_ptr(), _ptr(weight), _ptr(bias), _ptr(residual), out.data_ptr(), _ptr(ws), need.value, stream))
+    _on(dev, call)
+    return out
+
+
+class AdapterProjection:
+    """ee_adapter_*: a shared projection x w^T + bias and, beside it, the low-rank adapter of each request.  weight: bfloat16 [co, ci]; bias: float32 [co].
+    Room for `adapters` adapters of rank <= `rank`; load() puts one in (also between calls), unload() takes it out."""
+
+    def __init__(self, weight, bias=None, adapters=0, rank=16):
+        dev = weight.device
+        _tensor(weight, "weight", (torch.bfloat16,), dev)
+        _need(weight.dim() == 2 and weight.stride(1) == 1, "weight has to be [co, ci] with dense rows")
+        co, ci = weight.shape
+        if bias is not None:
+            _tensor(bias, "bias", (torch.float32,), dev)
+            _need(bias.shape == (co,) and bias.is_contiguous(), "bias has to be dense [co]")
+        self.device, self.ci, self.co, self.adapters, self.rank = dev, ci, co, adapters, rank
+        self._dims = AdapterDims(ci, co, adapters, rank)
+        packed, pool = C.c_int64(), C.c_int64()
+        _chk(_lib.ee_adapter_bytes(C.byref(self._dims), C.byref(packed), C.byref(pool)))
+        self._packed = torch.empty(packed.value, dtype=torch.uint8, device=dev)
+        self._pool = torch.zeros(pool.value, dtype=torch.uint8, device=dev)
+        _on(dev, lambda s: _chk(_lib.ee_adapter_pack(C.byref(self._dims), weight.data_ptr(), weight.stride(0), _ptr(bias), self._packed.data_ptr(), s)))
+
+    def load(self, i, a, b, scale=1.0):
+        """Adapter i becomes scale * b a (a: bfloat16 [r, ci], b: bfloat16 [co, r], r <= rank), for the calls behind this one on its stream."""
+        for t, name in ((a, "a"), (b, "b")):
+            _tensor(t, name, (torch.bfloat16,), self.device)
+            _need(t.dim() == 2 and t.stride(1) == 1 or t.shape[1:] == (1,), f"{name} has to have dense rows")
+        r = a.shape[0]
+        _need(a.shape == (r, self.ci) and b.shape == (self.co, r), "a has to be [r, ci] and b [co, r]")
+        _on(self.device, lambda s: _chk(_lib.ee_adapter_load(C.byref(self._dims), i, r, a.data_ptr(), a.stride(0), b.data_ptr(), b.stride(0), scale, self._pool.data_ptr(), s)))
+
+    def unload(self, i):
+        _on(self.device, lambda s: _chk(_lib.ee_adapter_load(C.byref(self._dims), i, 0, None, 0, None, 0, 0.0, self._pool.data_ptr(), s)))
+
+    def __call__(self, x, ids=None, offsets=None, out=None, dtype=torch.bfloat16):
+        """x: bfloat16 [slots, ..., ci] or, with offsets (int32 [slots + 1]), [rows, ci] with the rows of slot s at offsets[s]..offsets[s + 1]; ids: int32 [slots], the adapter of
+        every slot, outside [0, adapters): none.  Returns bfloat16 or float32 (dtype) with co in place of ci."""
+        dev = self.device
+        _tensor(x, "x", (torch.bfloat16,), dev)
+        if offsets is not None:
+            _tensor(offsets, "offsets", (torch.int32,), dev)
+            _need(x.dim() == 2 and offsets.dim() == 1 and offsets.numel() >= 1 and offsets.is_contiguous(), "offsets go with x [rows, ci]")
+            slots, per = offsets.numel() - 1, 0
+        b, inner, ci, sample, pixel = _pixels(x, "x")
+        if offsets is None:
+            slots, per = b, inner
+        if inner == 1:
+            pixel = sample
+        else:
+            _need(b <= 1 or sample == inner * pixel, "the rows of x have to lie one stride apart")
+        rows, ldx = b * inner, pixel if b * inner > 1 else ci
+        _need(ci == self.ci, "x has to have ci channels")
+        if ids is not None:
+            _tensor(ids, "ids", (torch.int32,), dev)
+            _need(ids.shape == (slots,) and ids.is_contiguous(), "ids has to be dense [slots]")
+        _need(dtype in (torch.bfloat16, torch.float32), "results are bfloat16 or float32", EE_ERR_UNSUPPORTED)
+        shape = x.shape[:-1] + (self.co,)
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=dev)
+            ldy = self.co
+        else:
+            _tensor(out, "out", (dtype,), dev)
+            _need(out.shape == shape, "out has to have the shape of x with co channels")
+            ob, oi, _, os_, op = _pixels(out, "out")
+            _need(oi == 1 or ob <= 1 or os_ == oi * op, "the rows of out have to lie one stride apart")
+            ldy = (os_ if oi == 1 else op) if ob * oi > 1 else self.co
+        need = C.c_int64()
+        _chk(_lib.ee_adapter_workspace(C.byref(self._dims), rows, C.byref(need)))
+
+        def call(stream):
+            ws = _workspace(need.value, dev)
+            c = AdapterCall(self._packed.data_ptr(), self._pool.data_ptr(), x.data_ptr(), out.data_ptr(), _ptr(ids), _ptr(offsets), ldx, ldy, rows, slots, per,
+                            int(dtype == torch.float32), _ptr(ws), need.value)
+            _chk(_lib.ee_adapter_project(C.byref(self._dims), C.byref(c), stream))
+        _on(dev, call)
+        return out
+
+
+def verify_draft(draft, target_probs, u, draft_probs=None, lengths=None):
+    """ee_verify_draft: (accepted int32 [b], tokens int32 [b, k + 1]) for draft int32 [b, k] against target_probs [b, k + 1, v] (float32 or bfloat16), drawn from draft_probs
+    [b, k, v] (same type; None: certain), with the random numbers u float32 [b, k + 1] in [0, 1).  lengths int32 [b]: drafts per sequence, < 0: an empty slot."""
+    dev = target_probs.device
+    _tensor(target_probs, "target_probs", (torch.float32, torch.bfloat16), dev)
+    _tensor(draft, "draft", (torch.int32,), dev)
+    _tensor(u, "u", (torch.float32,), dev)
+    _need(draft.dim() == 2 and target_probs.dim() == 3, "draft has to be [b, k], target_probs [b, k + 1, v]")
+    b, k = draft.shape
+    v = target_probs.shape[2]
+    _need(target_probs.shape[:2] == (b, k + 1) and u.shape == (b, k + 1), "target_probs and u have to have k + 1 rows a sequence")
+    dense = lambda t: t.shape[-1] <= 1 or t.stride(-1) == 1
+    _need(dense(target_probs) and dense(draft) and dense(u), "the last dimension has to be dense")
+    q_seq = q_row = 0
+    if draft_probs is not None:
+        _tensor(draft_probs, "draft_probs", (target_probs.dtype,), dev)
+        _need(draft_probs.shape == (b, k, v) and dense(draft_probs), "draft_probs has to be [b, k, v] with dense rows")
+        q_seq, q_row = draft_probs.stride(0), draft_probs.stride(1)
+    if lengths is not None:
+        _tensor(lengths, "lengths", (torch.int32,), dev)
+        _need(lengths.shape == (b,) and lengths.is_contiguous(), "lengths has to be dense [b]")
+    accepted = torch.empty(b, dtype=torch.int32, device=dev)
+    tokens = torch.empty(b, k + 1, dtype=torch.int32, device=dev)
+    need = C.c_int64()
+    _chk(_lib.ee_verify_workspace(b, k, v, C.byref(need)))
+
+    def call(stream):
+        ws = _workspace(need.value, dev)
+        c = VerifyCall(draft.data_ptr(), target_probs.data_ptr(), _ptr(draft_probs), u.data_ptr(), _ptr(lengths), accepted.data_ptr(), tokens.data_ptr(), draft.stride(0), u.stride(0),
+                       target_probs.stride(0), target_probs.stride(1), q_seq, q_row, b, k, v, int(target_probs.dtype == torch.float32), _ptr(ws), need.value)
+        _chk(_lib.ee_verify_draft(C.byref(c), stream))
+    _on(dev, call)
+    return accepted, tokens

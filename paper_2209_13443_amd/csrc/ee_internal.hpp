@@ -2,6 +2,7 @@
 #pragma once
 #include <utility>
 #include <hip/hip_runtime.h>
+#include <cmath>
 #include <cstring>
 #include <hip/hip_ext.h>
 
@@ -410,5 +411,40 @@ hipError_t launch_compact(const uint8_t* flag, const void* src, void* dst, const
                           int* b_rem_out, int* b_merged_out, hipStream_t s);
 // Admission: pool rows ids[k] -> slots [0, b)
 hipError_t launch_admit(const void* pool, void* dst, const int32_t* ids, int b, int64_t sample_bytes, hipStream_t s);
+
+// ---- operators that are calls of their own (kernels_norm.hip, kernels_adapter.hip, kernels_verify.hip) -----------------------------
+struct NormArgs {         // group norm with an activation; strides in elements, channels are neighbours
+    const void* x; const void* res; void* y;
+    const float* weight; const float* bias;
+    int64_t x_sample, x_pixel, res_sample, res_pixel, y_sample, y_pixel;
+    int dtype, act, b, pixels, c, groups, frac_bits, res_shift;
+    float eps;
+};
+bool group_norm_supported(const NormArgs& a);           // a group's channels fit a workgroup's columns
+bool group_norm_grid_fits(const NormArgs& a);
+size_t group_norm_workspace(const NormArgs& a);
+hipError_t launch_group_norm(const NormArgs& a, void* workspace, hipStream_t s);
+
+struct AdapterDims { int ci, co, adapters, rank; };
+struct AdapterCall {
+    const void* packed; const void* pool; const void* x; void* y; void* workspace;
+    const int* ids; const int* offsets;
+    int64_t ldx, ldy;
+    int rows, slots, per, out_f32;
+};
+int64_t adapter_weight_bytes(const AdapterDims& d);
+int64_t adapter_pool_bytes(const AdapterDims& d);
+int64_t adapter_workspace(const AdapterDims& d, int64_t rows);
+hipError_t launch_adapter_pack(const AdapterDims& d, const void* w, int64_t ldw, const float* bias, void* packed, hipStream_t s);
+hipError_t launch_adapter_load(const AdapterDims& d, int i, int rank, const void* a, int64_t lda, const void* b, int64_t ldb, float scale, void* pool, hipStream_t s);
+hipError_t launch_adapter_project(const AdapterDims& d, const AdapterCall& c, hipStream_t s);
+
+struct VerifyCall {       // strides in elements
+    const int* draft; const void* p; const void* q; const float* u; const int* lengths; int* accepted; int* tokens;
+    int64_t draft_row, u_row, p_seq, p_row, q_seq, q_row;
+    int b, k, v, f32;
+};
+size_t verify_workspace(const VerifyCall& c);
+hipError_t launch_verify(const VerifyCall& c, void* workspace, hipStream_t s);
 
 }  // namespace ee

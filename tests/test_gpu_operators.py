@@ -1,0 +1,528 @@
+"""The operators that are calls of their own (group norm with an activation, projection with per-request adapters, verification of
+drafted tokens) against their definitions in 64 bits, at the sizes, strides and values where they can go wrong.
+
+Tolerances: one rounding of the result (half a step, 2^-8 relative in bf16, 2^-24 in float32) plus what float sums of the given
+length may lose (a step of 2^-24 of the sum of the terms' magnitudes per addition, at the most)."""
+import sys
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+EPS = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}
+F32 = 2.0 ** -24
+
+
+def say(*a):
+    print(*a, flush=True)
+    sys.stdout.flush()
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available()
+    return torch
+
+
+@pytest.fixture(scope="module")
+def ee():
+    import paper_2209_13443_amd as ee
+    return ee
+
+
+# ---- group norm -------------------------------------------------------------------------------------------------------------------
+def norm_ref(torch, x, groups, w, b, eps, act, res, f=0, rs=0):
+    """(result, bound) in 64 bits; x [b, p, c]"""
+    n_b, pix, c = x.shape
+    cpg = c // groups
+    w = torch.ones(c, dtype=torch.float64, device=x.device) if w is None else w.double()
+    b = torch.zeros(c, dtype=torch.float64, device=x.device) if b is None else b.double()
+    if x.dtype == torch.int8:
+        xi = x.long().view(n_b, pix, groups, cpg)
+        n = pix * cpg
+        s1, s2 = xi.sum((1, 3), keepdim=True), (xi * xi).sum((1, 3), keepdim=True)
+        var = (n * s2 - s1 * s1).double() / float(n) ** 2
+        t = (n * xi - s1).double() * (w.view(groups, cpg) * 2.0 ** f / (n * (var + np.float32(eps)).sqrt())) + (b.view(groups, cpg) * 2.0 ** f + 0.5)
+        t = t.view(x.shape)
+        if res is not None:
+            t = t + res.double() * 2.0 ** rs
+        lo, hi = {"none": (-128, 127), "relu": (0, 127), "relu6": (0, min(127, 6 * 2 ** f))}[act]
+        return t.floor().clamp(lo, hi).to(torch.int8), None
+    xd = x.double().view(n_b, pix, groups, cpg)
+    mean = xd.mean((1, 3), keepdim=True)
+    a = w.view(groups, cpg) / ((xd - mean).square().mean((1, 3), keepdim=True) + np.float32(eps)).sqrt()
+    y = ((xd - mean) * a + b.view(groups, cpg)).view(x.shape)
+    # the mean and the variance from at most a few dozen additions behind one another each, of numbers as large as the largest
+    size = (((xd - mean).abs() + xd.abs().amax((1, 3), keepdim=True)) * a.abs()).view(x.shape) + b.abs()
+    if res is not None:
+        y = y + res.double()
+        size = size + res.double().abs()
+    y = {"none": lambda v: v, "relu": lambda v: v.clamp(min=0), "relu6": lambda v: v.clamp(0, 6), "silu": lambda v: v * torch.sigmoid(v)}[act](y)
+    return y, EPS["bf16"] * y.abs() + 128 * F32 * size + 1e-30
+
+
+NORM_SHAPES = [  # b, h, w, c, groups
+    (1, 1, 1, 8, 8), (1, 1, 1, 1, 1), (3, 1, 1, 64, 4), (2, 7, 7, 512, 32), (5, 3, 5, 24, 3), (2, 9, 11, 96, 12), (3, 5, 7, 33, 3), (2, 13, 13, 40, 20), (1, 56, 56, 64, 32),
+    (2, 31, 33, 288, 24), (1, 100, 100, 16, 2), (1, 1, 1, 8192, 1), (2, 2, 3, 1030, 1030), (1, 130, 120, 64, 32), (1, 300, 260, 32, 4), (2, 70, 70, 1024, 1), (1, 67, 61, 7, 7), (3, 20, 20, 1000, 5),
+    (2, 17, 19, 272, 16), (1, 90, 91, 80, 4), (1, 70, 60, 56, 2), (1, 65, 66, 2056, 4)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "int8"])
+@pytest.mark.parametrize("shape", NORM_SHAPES)
+def test_group_norm_shapes(torch, ee, shape, dtype):
+    b, h, w, c, groups = shape
+    g = torch.Generator(device="cuda").manual_seed(h * w + c)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    kind = torch.bfloat16 if dtype == "bf16" else torch.int8
+    x = (rnd(b, h, w, c) * 2 + rnd(c)).to(kind) if dtype == "bf16" else (rnd(b, h, w, c) * 40 + 10 * rnd(c)).clamp(-128, 127).to(kind)
+    res = rnd(b, h, w, c).mul_(30 if dtype == "int8" else 1).clamp(-128, 127).to(kind)
+    wt, bs = 1 + 0.3 * rnd(c), 0.5 * rnd(c)
+    for act, r, aff in (("none", None, False), ("relu", res, True), ("silu" if dtype == "bf16" else "relu6", None, True)):
+        say(f"[case] norm {shape} {dtype} {act} residual {r is not None}")
+        got = ee.group_norm(x, groups, wt if aff else None, bs if aff else None, act=act, residual=r, frac_bits=4, res_shift=-1)
+        torch.cuda.synchronize()
+        flat = lambda t: None if t is None else t.reshape(b, h * w, c)
+        ref, tol = norm_ref(torch, flat(x), groups, wt if aff else None, bs if aff else None, 1e-5, act, flat(r), 4, -1)
+        got = got.reshape(b, h * w, c)
+        if tol is None:
+            assert torch.equal(got, ref), f"{int((got != ref).sum())} of {ref.numel()} differ"
+        else:
+            off = (got.double() - ref).abs() - tol
+            assert float(off.max()) <= 0, f"off by {float(off.max())} more than the bound"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "int8"])
+def test_group_norm_slices_strides_and_in_place(torch, ee, dtype):
+    kind = torch.bfloat16 if dtype == "bf16" else torch.int8
+    g = torch.Generator(device="cuda").manual_seed(3)
+    wide = (torch.randn(4, 6, 5, 96, device="cuda", generator=g) * 20).to(kind)
+    for c0, c1, groups in ((0, 32, 4), (32, 80, 3), (1, 34, 3), (90, 96, 2)):
+        say(f"[case] slice {c0}:{c1} {dtype}")
+        x = wide[:, :, :, c0:c1]
+        ref, tol = norm_ref(torch, x.reshape(4, 30, c1 - c0), groups, None, None, 1e-5, "relu", None, 5)
+        out = wide.clone()
+        got = ee.group_norm(x, groups, act="relu", frac_bits=5, out=out[..., c0:c1])
+        plain = ee.group_norm(x.contiguous(), groups, act="relu", frac_bits=5)
+        here = wide.clone()
+        ee.group_norm(here[..., c0:c1], groups, act="relu", frac_bits=5, out=here[..., c0:c1])
+        torch.cuda.synchronize()
+        assert (torch.equal(got.reshape(ref.shape), ref) if tol is None else bool(((got.reshape(ref.shape).double() - ref).abs() <= tol).all()))
+        near = lambda a, b: torch.equal(a, b) if dtype == "int8" else bool(((a.double() - b.double()).abs() <= 2 * tol.view(a.shape)).all())
+        assert near(plain, got) and near(here[..., c0:c1], got)
+        keep = torch.ones(96, dtype=torch.bool, device="cuda")
+        keep[c0:c1] = False
+        assert torch.equal(out[..., keep], wide[..., keep]) and torch.equal(here[..., keep], wide[..., keep])     # the rest of the wide tensor is left alone
+    # every other sample; a large tensor (two launches) in place
+    x = (torch.randn(4, 90, 90, 64, device="cuda", generator=g) * 20).to(kind)
+    ref, tol = norm_ref(torch, x[::2].reshape(2, 8100, 64), 8, None, None, 1e-5, "none", None, 5)
+    got = x.clone()
+    ee.group_norm(got[::2], 8, frac_bits=5, out=got[::2])
+    assert (torch.equal(got[::2].reshape(ref.shape), ref) if tol is None else bool(((got[::2].reshape(ref.shape).double() - ref).abs() <= tol).all()))
+    assert torch.equal(got[1::2], x[1::2])
+
+
+@pytest.mark.parametrize("pixels", [1, 49, 4100, 40000])
+def test_group_norm_values(torch, ee, pixels):
+    """Constant groups, a mean far from zero, extreme int8 values, a NaN and an infinity that stay in their own group and sample."""
+    c, groups = 32, 4
+    bias = torch.linspace(-1, 1, c, device="cuda")
+    const = torch.full((2, pixels, c), 3.0, device="cuda").to(torch.bfloat16)
+    got = ee.group_norm(const, groups, None, bias)
+    assert torch.equal(got, bias.to(torch.bfloat16).expand_as(got))
+    q = torch.full((2, pixels, c), -128, dtype=torch.int8, device="cuda")
+    half = torch.full((c,), 0.5, device="cuda")
+    assert bool((ee.group_norm(q, groups, None, half, frac_bits=0) == 1).all())                  # floor(0.5 + 0.5): on the border, on every machine
+    g = torch.Generator(device="cuda").manual_seed(pixels)
+    ends = torch.where(torch.rand(2, pixels, c, device="cuda", generator=g) < 0.5, -128, 127).to(torch.int8)
+    ref, _ = norm_ref(torch, ends, groups, None, bias, 1e-5, "none", None, 5)
+    assert torch.equal(ee.group_norm(ends, groups, None, bias, frac_bits=5), ref)
+    far = (300 + torch.randn(2, pixels, c, device="cuda", generator=g) * 4).to(torch.bfloat16)
+    ref, tol = norm_ref(torch, far, groups, None, bias, 1e-5, "none", None)
+    assert bool(((ee.group_norm(far, groups, None, bias).double() - ref).abs() <= tol).all())
+    x = torch.randn(3, pixels, c, device="cuda", generator=g).to(torch.bfloat16)
+    clean = ee.group_norm(x, groups, None, bias, act="silu")
+    x[1, pixels // 2, 9] = float("nan")
+    x[2, pixels - 1, 0] = float("inf")
+    got = ee.group_norm(x, groups, None, bias, act="silu")
+    assert bool(got[1, :, 8:16].isnan().all()) and bool(got[2, :, :8].isnan().all())
+    same = torch.ones_like(got, dtype=torch.bool)
+    same[1, :, 8:16] = False
+    same[2, :, :8] = False
+    assert torch.equal(got[same], clean[same])
+    assert ee.group_norm(x[:0], groups).shape == (0, pixels, c)
+
+
+def test_group_norm_bits_as_int16_and_refusals(torch, ee):
+    x = torch.randn(2, 4, 4, 16, device="cuda").to(torch.bfloat16)
+    got = ee.group_norm(x.view(torch.int16), 4, act="relu")
+    assert got.dtype == torch.int16 and torch.equal(got.view(torch.bfloat16), ee.group_norm(x, 4, act="relu"))
+
+    def refused(code, *a, **k):
+        with pytest.raises(ee.EEError) as e:
+            ee.group_norm(*a, **k)
+        assert e.value.code == code, e.value
+    refused(ee.EE_ERR_ARG, x, 3)
+    refused(ee.EE_ERR_ARG, x, 0)
+    refused(ee.EE_ERR_ARG, x, 4, act="gelu")
+    refused(ee.EE_ERR_ARG, x, 4, eps=float("nan"))
+    refused(ee.EE_ERR_ARG, x, 4, eps=-1.0)
+    refused(ee.EE_ERR_UNSUPPORTED, x.to(torch.int8), 4, act="silu")
+    refused(ee.EE_ERR_UNSUPPORTED, x.float(), 4)
+    refused(ee.EE_ERR_ARG, x, 4, weight=torch.ones(8, device="cuda"))
+    refused(ee.EE_ERR_ARG, x, 4, weight=torch.ones(16))
+    refused(ee.EE_ERR_UNSUPPORTED, x, 4, weight=torch.ones(16, device="cuda", dtype=torch.bfloat16))
+    refused(ee.EE_ERR_ARG, x, 4, residual=x[:1])
+    refused(ee.EE_ERR_ARG, x.permute(0, 3, 1, 2), 4)
+    refused(ee.EE_ERR_ARG, x.transpose(1, 2)[:, :, :3], 4)                     # pixels that are no one stride apart
+    refused(ee.EE_ERR_UNSUPPORTED, torch.zeros(1, 1, 8200, device="cuda", dtype=torch.bfloat16), 1)
+
+
+# ---- projection with adapters -----------------------------------------------------------------------------------------------------------
+def project_ref(torch, x, w, bias, ad, rows_ids, out):
+    """(result, bound) in 64 bits; ad: list of (a, b, scale); x [rows, ci]"""
+    xd, wd = x.double(), w.double()
+    y, size = xd @ wd.T, xd.abs() @ wd.abs().T
+    if bias is not None:
+        y, size = y + bias.double(), size + bias.double().abs()
+    extra = torch.zeros_like(y)
+    for i, (a, b, s) in enumerate(ad):
+        at = (rows_ids == i).nonzero()[:, 0]
+        if at.numel() and a is not None:
+            y[at] += s * ((xd[at] @ a.double().T) @ b.double().T)
+            extra[at] = abs(s) * ((xd[at].abs() @ a.double().abs().T) @ b.double().abs().T)
+    ci = x.shape[1]
+    # float sums of ci terms, of the rank's for the adapter (whose inner sums are rounded to 2^-18, or 2^-24 for float results)
+    return y, EPS[out] * y.abs() + (ci + 8) * F32 * (size + extra) + ({"bf16": 2.0 ** -18, "fp32": F32}[out] + 520 * F32) * extra + 1e-30
+
+
+def adapters_of(torch, g, n, r, ci, co):
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    return [((rnd(r, ci) / ci ** 0.5).bfloat16(), (rnd(co, r) / r ** 0.5).bfloat16(), 0.5 + i) for i in range(n)]
+
+
+PROJECTIONS = [  # slots, per, ci, co, rank, adapters
+    (1, 1, 8, 8, 1, 1), (1, 1, 1, 1, 1, 2), (3, 1, 33, 5, 4, 2), (12, 1, 512, 1000, 16, 5), (64, 1, 2048, 100, 8, 24), (70, 1, 100, 300, 10, 70), (5, 49, 256, 64, 32, 3), (7, 9, 72, 130, 128, 4),
+    (2, 200, 320, 512, 64, 2), (40, 16, 96, 1001, 16, 7), (300, 1, 128, 257, 33, 9), (2, 1, 4096, 4096, 16, 2), (33, 4, 1000, 96, 256, 2), (4, 70, 64, 32, 16, 0), (16, 33, 513, 65, 5, 16),
+    (17, 1, 256, 2048, 16, 17), (130, 3, 64, 640, 40, 30)]
+
+
+@pytest.mark.parametrize("case", PROJECTIONS)
+def test_adapter_projection_shapes(torch, ee, case):
+    slots, per, ci, co, r, n = case
+    g = torch.Generator(device="cuda").manual_seed(ci * 7 + co)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    w, bias, ad = (rnd(co, ci) / ci ** 0.5).bfloat16(), rnd(co), adapters_of(torch, g, n, r, ci, co)
+    proj = ee.AdapterProjection(w, bias, adapters=n, rank=r)
+    for i, (a, b, s) in enumerate(ad):
+        proj.load(i, a, b, s)
+    x = rnd(slots, per, ci).bfloat16()
+    ids = torch.randint(-2, n + 2, (slots,), device="cuda", generator=g, dtype=torch.int32)            # some in front of and behind the adapters: none
+    for out in ("bf16", "fp32"):
+        say(f"[case] project {case} {out}")
+        got = proj(x, ids if n else None, dtype=torch.bfloat16 if out == "bf16" else torch.float32)
+        torch.cuda.synchronize()
+        ref, tol = project_ref(torch, x.view(-1, ci), w, bias, ad, ids.repeat_interleave(per), out)
+        off = (got.view(-1, co).double() - ref).abs() - tol
+        assert got.shape == (slots, per, co) and float(off.max()) <= 0, f"off by {float(off.max())} more than the bound"
+
+
+@pytest.mark.parametrize("ci,co,r", [(64, 96, 16), (72, 33, 8), (45, 200, 64)])
+@pytest.mark.parametrize("lengths", [(0, 5, 0, 1, 40, 0), (1,), (0, 0), (200, 1, 1, 130), (3,) * 50])
+def test_adapter_projection_packed_rows(torch, ee, ci, co, r, lengths):
+    """Runs of different lengths, empty ones too; rows in front of the first and behind the last slot are left as they were and may hold anything."""
+    g = torch.Generator(device="cuda").manual_seed(sum(lengths) + ci)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    n, front, behind = 4, 3, 37
+    w, ad = (rnd(co, ci) / ci ** 0.5).bfloat16(), adapters_of(torch, g, n, r, ci, co)
+    proj = ee.AdapterProjection(w, None, adapters=n, rank=r)
+    for i, (a, b, s) in enumerate(ad):
+        proj.load(i, a, b, s)
+    rows = front + sum(lengths) + behind
+    x = rnd(rows, ci).bfloat16()
+    x[:front] = float("nan")
+    x[rows - behind:] = float("inf")
+    offsets = torch.tensor([front + sum(lengths[:i]) for i in range(len(lengths) + 1)], dtype=torch.int32, device="cuda")
+    ids = torch.randint(-1, n, (len(lengths),), device="cuda", generator=g, dtype=torch.int32)
+    out = torch.full((rows, co), 7.0, device="cuda").bfloat16()
+    say(f"[case] packed {lengths} {ci} {co} {r}")
+    assert proj(x, ids, offsets=offsets, out=out) is out
+    torch.cuda.synchronize()
+    mine = slice(front, rows - behind)
+    assert bool((out[:front] == 7).all()) and bool((out[rows - behind:] == 7).all())
+    if sum(lengths):
+        ref, tol = project_ref(torch, x[mine], w, None, ad, ids.repeat_interleave(torch.tensor(lengths, device="cuda")), "bf16")
+        assert bool(((out[mine].double() - ref).abs() <= tol).all())
+
+
+def test_adapter_projection_strides_loading_and_rows_apart(torch, ee):
+    g = torch.Generator(device="cuda").manual_seed(11)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    ci, co, n = 120, 72, 3
+    wide = rnd(co, ci + 9).bfloat16()
+    w, ad = wide[:, 3:3 + ci], adapters_of(torch, g, n, 8, ci, co)
+    proj = ee.AdapterProjection(w, None, adapters=n, rank=12)
+    ids = torch.arange(20, device="cuda", dtype=torch.int32) % (n + 1)
+    base = proj(rnd(20, ci).bfloat16(), ids)                                   # nothing loaded: no adapter adds anything
+    assert bool(base.isfinite().all())
+    for i, (a, b, s) in enumerate(ad):
+        proj.load(i, a, b, s)
+    for lead, step in ((0, ci), (0, ci + 8), (8, ci + 24), (1, ci + 5)):
+        big = rnd(20, lead + step + 8).bfloat16()
+        x = big[:, lead:lead + ci]
+        out = torch.full((20, co + 11), 5.0, device="cuda")
+        say(f"[case] rows {lead} {step}")
+        proj(x, ids, out=out[:, 4:4 + co], dtype=torch.float32)
+        ref, tol = project_ref(torch, x, w, None, ad, ids, "fp32")
+        assert bool(((out[:, 4:4 + co].double() - ref).abs() <= tol).all()) and bool((out[:, :4] == 5).all()) and bool((out[:, 4 + co:] == 5).all())
+    # a smaller adapter in place of a larger one, one taken out, between calls
+    a, b, _ = adapters_of(torch, g, 1, 2, ci, co)[0]
+    proj.load(1, a, b, -3.0)
+    proj.unload(2)
+    now = [ad[0], (a, b, -3.0), (None, None, 0.0)]
+    x = rnd(20, ci).bfloat16()
+    ref, tol = project_ref(torch, x, w, None, now, ids, "bf16")
+    assert bool(((proj(x, ids).double() - ref).abs() <= tol).all())
+    # a row that is not finite stays alone, whatever adapter it has
+    clean = proj(x, ids)
+    for row in (0, 1, 19):
+        bad = x.clone()
+        bad[row, 5] = float("nan")
+        got = proj(bad, ids)
+        rest = torch.arange(20, device="cuda") != row
+        assert bool(got[row].isnan().all()) and torch.equal(got[rest], clean[rest])
+
+
+def test_adapter_projection_refusals(torch, ee):
+    w = torch.zeros(32, 16, device="cuda", dtype=torch.bfloat16)
+    proj = ee.AdapterProjection(w, adapters=2, rank=4)
+    x = torch.zeros(6, 16, device="cuda", dtype=torch.bfloat16)
+    ids = torch.zeros(6, device="cuda", dtype=torch.int32)
+
+    def refused(code, f, *a, **k):
+        with pytest.raises(ee.EEError) as e:
+            f(*a, **k)
+        assert e.value.code == code, e.value
+    refused(ee.EE_ERR_ARG, proj, x)                                            # adapters, and no ids
+    refused(ee.EE_ERR_ARG, proj, x, ids[:5])
+    refused(ee.EE_ERR_UNSUPPORTED, proj, x, ids.long())
+    refused(ee.EE_ERR_ARG, proj, x[:, :8], ids)
+    refused(ee.EE_ERR_UNSUPPORTED, proj, x.float(), ids)
+    refused(ee.EE_ERR_UNSUPPORTED, proj, x, ids, dtype=torch.float16)
+    refused(ee.EE_ERR_ARG, proj, x, ids, out=torch.zeros(6, 31, device="cuda", dtype=torch.bfloat16))
+    refused(ee.EE_ERR_ARG, proj, x, ids, offsets=torch.zeros(6, device="cuda", dtype=torch.int32))
+    refused(ee.EE_ERR_ARG, proj, x.cpu(), ids)
+    refused(ee.EE_ERR_ARG, proj.load, 2, x[:4], w[:, :4])
+    refused(ee.EE_ERR_ARG, proj.load, 0, x[:5], w[:, :5])
+    refused(ee.EE_ERR_ARG, proj.load, 0, x[:4], w[:, :3])
+    refused(ee.EE_ERR_OVERFLOW, ee.AdapterProjection, w, adapters=2, rank=300)
+    assert proj(x[:0], ids[:0]).shape == (0, 32)
+
+
+# ---- verification -----------------------------------------------------------------------------------------------------------------------
+def verify_ref(draft, p, q, u, lengths):
+    """numpy, 64 bits; p [b, k + 1, v] float64"""
+    b, k = draft.shape
+    v = p.shape[2]
+    accepted, tokens = np.zeros(b, np.int32), np.full((b, k + 1), -1, np.int32)
+    fine = lambda w: np.where((w > 0) & np.isfinite(w), w, 0.0)
+    for i in range(b):
+        m = k if lengths is None else min(int(lengths[i]), k)
+        if m < 0:
+            continue
+        n = 0
+        while n < m and 0 <= draft[i, n] < v and float(u[i, n]) * (1.0 if q is None else q[i, n, draft[i, n]]) < p[i, n, draft[i, n]]:
+            tokens[i, n] = draft[i, n]
+            n += 1
+        w = p[i, n]
+        if n < m:
+            less = np.zeros(v) if q is None else q[i, n]
+            w = fine(w - less)
+            if q is None and 0 <= draft[i, n] < v:
+                w[draft[i, n]] = 0.0
+            if not w.sum() > 0:
+                w = p[i, n]
+        w = fine(w)
+        accepted[i] = n
+        if w.sum() > 0:
+            cum = np.cumsum(w)
+            over = np.nonzero((cum > float(u[i, k]) * cum[-1]) & (w > 0))[0]
+            tokens[i, n] = over[0] if over.size else np.nonzero(w > 0)[0][-1]
+    return accepted, tokens
+
+
+def check_verify(torch, ee, draft, p, q, u, lengths, what):
+    say(f"[case] verify {what}")
+    got = ee.verify_draft(draft, p, u, draft_probs=q, lengths=lengths)
+    again = ee.verify_draft(draft, p, u, draft_probs=q, lengths=lengths)
+    torch.cuda.synchronize()
+    host = lambda t: None if t is None else t.double().cpu().numpy()
+    ref = verify_ref(draft.cpu().numpy(), host(p), host(q), u.cpu().numpy(), None if lengths is None else lengths.cpu().numpy())
+    assert np.array_equal(got[0].cpu().numpy(), ref[0]), what
+    bad = np.nonzero(got[1].cpu().numpy() != ref[1])
+    assert bad[0].size == 0, f"{what}: {[(int(i), int(j), int(got[1][i, j]), int(ref[1][i, j])) for i, j in zip(*bad)][:5]}"
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+    return got
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("b,k,v", [(1, 0, 1), (1, 1, 1), (4, 3, 2), (7, 4, 100), (16, 5, 1000), (3, 70, 37), (9, 2, 4096), (9, 2, 4097), (5, 8, 33001), (2, 1, 128256), (1, 2, 1100000)])
+def test_verify_draft_shapes(torch, ee, b, k, v, dtype):
+    kind = torch.float32 if dtype == "fp32" else torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(b * 100 + k * 10 + v)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    logits = 2 * rnd(b, k + 1, v)
+    p = torch.softmax(logits, -1).to(kind)
+    weak = logits[:, :k] + 0.5 * rnd(b, k, v)
+    q = torch.softmax(weak, -1).to(kind)
+    draft = (weak - torch.empty_like(weak).exponential_(generator=g).log_()).argmax(-1).int() if k else torch.zeros(b, 0, dtype=torch.int32, device="cuda")
+    u = torch.rand(b, k + 1, device="cuda", generator=g)
+    lengths = torch.randint(-1, k + 2, (b,), device="cuda", generator=g, dtype=torch.int32)
+    for qq in (q, None):
+        for ll in (None, lengths):
+            check_verify(torch, ee, draft, p, qq, u, ll, f"{b} {k} {v} {dtype} q {qq is not None} lengths {ll is not None}")
+
+
+def test_verify_draft_strange_values(torch, ee):
+    """Rows of zeros, NaN and infinities, residuals with nothing in them, drafts outside the vocabulary, random numbers at both ends, views."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    b, k, v = 12, 3, 5000
+    p = torch.softmax(torch.randn(b, k + 1, v, device="cuda", generator=g), -1)
+    q = torch.softmax(torch.randn(b, k, v, device="cuda", generator=g), -1)
+    draft = torch.randint(0, v, (b, k), device="cuda", generator=g, dtype=torch.int32)
+    u = torch.rand(b, k + 1, device="cuda", generator=g)
+    p[0] = 0
+    p[1] = float("nan")
+    p[2, :, 100] = float("inf")
+    p[3, :, 7] = float("nan")
+    q[4] = p[4, :k]                      # refused only where u is 1: nothing is left, p is drawn from
+    u[4, :k] = 1.0
+    q[5] = float("nan")
+    draft[6, 0], draft[7, 1], draft[8, 2] = -1, v, 2 ** 31 - 1
+    u[9] = 0.0
+    u[10] = 1.0
+    p[11] = 0
+    p[11, :, 4321] = 0.25                # one entry, behind the first chunk
+    for qq in (q, None):
+        check_verify(torch, ee, draft, p, qq, u, None, f"strange {qq is not None}")
+        check_verify(torch, ee, draft, p, qq, torch.full_like(u, float("nan")), None, f"no numbers {qq is not None}")
+    # views: rows of wider tensors, odd starts
+    for kind in (torch.float32, torch.bfloat16):
+        wide_p, wide_q = torch.rand(b, k + 3, v + 13, device="cuda", generator=g).to(kind), torch.rand(b, k + 3, v + 13, device="cuda", generator=g).to(kind)
+        wide_u, wide_d = torch.rand(b, k + 5, device="cuda", generator=g), torch.randint(0, v, (b, k + 5), device="cuda", generator=g, dtype=torch.int32)
+        check_verify(torch, ee, wide_d[:, 2:2 + k], wide_p[:, 1:k + 2, 3:3 + v], wide_q[:, 2:k + 2, 5:5 + v], wide_u[:, 1:k + 2], None, f"views {kind}")
+        check_verify(torch, ee, wide_d[:, 2:2 + k], wide_p[:1, 1:2, 3:3 + v].expand(b, k + 1, v), None, wide_u[:, 1:k + 2], None, f"one row for all {kind}")
+
+
+def test_verify_draft_gives_the_targets_distribution(torch, ee):
+    """Whatever the draft, the first token that comes out has the target's probabilities: 400,000 sequences, each count within 6 standard deviations."""
+    n, v = 400_000, 6
+    g = torch.Generator(device="cuda").manual_seed(1)
+    p1 = torch.tensor([0.4, 0.05, 0.25, 0.0, 0.2, 0.1], device="cuda")
+    q1 = torch.tensor([0.1, 0.3, 0.25, 0.2, 0.15, 0.0], device="cuda")
+    draft = torch.multinomial(q1, n, replacement=True, generator=g).int()[:, None]
+    u = torch.rand(n, 2, device="cuda", generator=g)
+    _, tokens = ee.verify_draft(draft, p1.expand(n, 2, v), u, draft_probs=q1.expand(n, 1, v))
+    count = torch.bincount(tokens[:, 0].long(), minlength=v).double().cpu().numpy()
+    p = p1.double().cpu().numpy()
+    assert np.all(np.abs(count - n * p) <= 6 * np.sqrt(n * p * (1 - p)))
+
+
+def test_verify_draft_refusals(torch, ee):
+    p, q = torch.zeros(2, 4, 9, device="cuda"), torch.zeros(2, 3, 9, device="cuda")
+    d, u = torch.zeros(2, 3, device="cuda", dtype=torch.int32), torch.zeros(2, 4, device="cuda")
+
+    def refused(code, *a, **k):
+        with pytest.raises(ee.EEError) as e:
+            ee.verify_draft(*a, **k)
+        assert e.value.code == code, e.value
+    refused(ee.EE_ERR_UNSUPPORTED, d.long(), p, u)
+    refused(ee.EE_ERR_UNSUPPORTED, d, p.half(), u)
+    refused(ee.EE_ERR_UNSUPPORTED, d, p, u, draft_probs=q.bfloat16())
+    refused(ee.EE_ERR_ARG, d, p[:, :3], u)
+    refused(ee.EE_ERR_ARG, d, p, u[:, :3])
+    refused(ee.EE_ERR_ARG, d, p, u, draft_probs=p)
+    refused(ee.EE_ERR_ARG, d, p, u, lengths=torch.zeros(3, device="cuda", dtype=torch.int32))
+    refused(ee.EE_ERR_ARG, d.cpu(), p, u)
+    a, t = ee.verify_draft(d[:0], p[:0], u[:0])
+    assert a.shape == (0,) and t.shape == (0, 4)
+
+
+# ---- streams, graphs, all together --------------------------------------------------------------------------------------------------------
+def chain(ee, s):
+    """The end of a step: features normalised, an early and a last head with each request's adapter, the early exit's tokens verified by the last one."""
+    f = ee.group_norm(s["x"], 8, s["gw"], s["gb"], act="silu")
+    early, last = s["early"](f[:, :-1].contiguous(), s["ids"], dtype=s["torch"].float32), s["last"](f, s["ids"], dtype=s["torch"].float32)
+    q, p = s["torch"].softmax(early, -1), s["torch"].softmax(last, -1)
+    accepted, tokens = ee.verify_draft(s["draft"], p, s["u"], draft_probs=q, lengths=s["lengths"])
+    return f, early, last, p, q, accepted, tokens
+
+
+def chain_state(torch, ee, seed, b=9, k=4, c=128, v=700):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    s = dict(torch=torch, x=(2 * rnd(b, k + 1, c)).bfloat16(), gw=1 + 0.2 * rnd(c), gb=0.1 * rnd(c), ids=torch.randint(-1, 3, (b,), device="cuda", generator=g, dtype=torch.int32),
+             draft=torch.randint(0, v, (b, k), device="cuda", generator=g, dtype=torch.int32), u=torch.rand(b, k + 1, device="cuda", generator=g) ** 4,
+             lengths=torch.randint(0, k + 1, (b,), device="cuda", generator=g, dtype=torch.int32))
+    w = (rnd(v, c) / c ** 0.5).bfloat16()
+    for name, noise in (("early", 0.1), ("last", 0.0)):
+        wn = (w.float() + noise * rnd(v, c) / c ** 0.5).bfloat16()
+        s[name] = ee.AdapterProjection(wn, rnd(v), adapters=3, rank=8)
+        s[name + "_w"], s[name + "_ad"] = wn, adapters_of(torch, g, 3, 8, c, v)
+        for i, (a, bb, sc) in enumerate(s[name + "_ad"]):
+            s[name].load(i, a, bb, sc)
+    return s
+
+
+def test_chain_of_the_three_and_compaction(torch, ee):
+    """Norm, heads with adapters and verification as a step uses them, then the library's compaction takes out the sequences whose drafts were all accepted."""
+    import workloads as W
+    s = chain_state(torch, ee, 21)
+    f, early, last, p, q, accepted, tokens = chain(ee, s)
+    ref, tol = norm_ref(torch, s["x"], 8, s["gw"], s["gb"], 1e-5, "silu", None)
+    assert bool(((f.double() - ref).abs() <= tol).all())
+    want = verify_ref(s["draft"].cpu().numpy(), p.double().cpu().numpy(), q.double().cpu().numpy(), s["u"].cpu().numpy(), s["lengths"].cpu().numpy())
+    assert np.array_equal(accepted.cpu().numpy(), want[0]) and np.array_equal(tokens.cpu().numpy(), want[1])
+    blob = W.load_net("tiny_bf16")
+    eng = ee.Engine(blob, 16)
+    act = torch.randint(0, 100, (9,) + blob.stage_out_shape(0), device="cuda", dtype=torch.int16)
+    flags = (accepted == s["lengths"]).to(torch.uint8)
+    left, ids, b_rem, _ = eng.compact_refill(0, flags, act, s["ids"])
+    keep = flags == 0
+    assert b_rem == int(keep.sum()) and torch.equal(left, act[keep]) and torch.equal(ids, s["ids"][keep])
+    eng.close()
+
+
+def test_operators_on_another_stream_and_in_graphs(torch, ee):
+    """Two graphs captured from the same handles, replayed in turn with eager work between, equal to eager results on new inputs every time; another stream than the default."""
+    states = [chain_state(torch, ee, seed, b=b) for seed, b in ((1, 9), (2, 40))]
+    big = [torch.randn(2, 96, 96, 64, device="cuda").bfloat16() for _ in states]                      # two launches and a workspace
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs, outs = [], []
+    with torch.cuda.stream(side):
+        for s, x in zip(states, big):
+            chain(ee, s)
+            ee.group_norm(x, 32)
+    torch.cuda.synchronize()
+    for s, x in zip(states, big):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(chain(ee, s) + (ee.group_norm(x, 32),))
+        graphs.append(graph)
+    for turn in range(4):
+        g = torch.Generator(device="cuda").manual_seed(100 + turn)
+        for s, x in zip(states, big):
+            s["x"].copy_(2 * torch.randn(s["x"].shape, device="cuda", generator=g))
+            s["u"].copy_(torch.rand(s["u"].shape, device="cuda", generator=g))
+            s["ids"].copy_(torch.randint(-1, 3, s["ids"].shape, device="cuda", generator=g))
+            x.copy_(torch.randn(x.shape, device="cuda", generator=g))
+        for n in ((0, 1), (1, 0))[turn % 2]:
+            graphs[n].replay()
+        with torch.cuda.stream(side):
+            side.wait_stream(torch.cuda.default_stream())
+            eager = [chain(ee, s) + (ee.group_norm(x, 32),) for s, x in zip(states, big)]
+        torch.cuda.synchronize()
+        for got, want in zip(outs, eager):
+            for a, b in zip(got, want):
+                assert torch.equal(a, b), f"turn {turn}"

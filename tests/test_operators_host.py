@@ -1,0 +1,106 @@
+"""What the operators that need no context refuse, and the sizes they ask for: through the C ABI, without a GPU."""
+import ctypes as C
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def ee():
+    import paper_2209_13443_amd as ee
+    return ee
+
+
+def norm(ee, **k):
+    d = dict(dtype=ee.EE_BF16, act=0, b=2, pixels=49, c=64, groups=8, frac_bits=0, res_shift=0, eps=1e-5, pad_=0, x_sample=49 * 64, x_pixel=64, res_sample=0, res_pixel=0,
+             y_sample=49 * 64, y_pixel=64)
+    d.update(k)
+    return ee.NormDesc(**d)
+
+
+P = 4096        # stands for device memory: these calls end before they use it
+
+
+def test_group_norm_refuses(ee):
+    lib, n = ee.raw(), C.c_int64(-1)
+    bytes_of = lambda d: lib.ee_group_norm_workspace(C.byref(d), C.byref(n))
+    assert lib.ee_group_norm_workspace(None, C.byref(n)) == ee.EE_ERR_ARG and lib.ee_group_norm_workspace(C.byref(norm(ee)), None) == ee.EE_ERR_ARG
+    assert bytes_of(norm(ee)) == ee.EE_OK and n.value == 0
+    assert bytes_of(norm(ee, pixels=1 << 20)) == ee.EE_OK and n.value > 0
+    assert bytes_of(norm(ee, pixels=1 << 20, b=0)) == ee.EE_OK and n.value == 0
+    for code, bad in [(ee.EE_ERR_ARG, dict(groups=0)), (ee.EE_ERR_ARG, dict(groups=7)), (ee.EE_ERR_ARG, dict(c=0)), (ee.EE_ERR_ARG, dict(b=-1)), (ee.EE_ERR_ARG, dict(pixels=-1)),
+                      (ee.EE_ERR_ARG, dict(eps=-1e-5)), (ee.EE_ERR_ARG, dict(eps=float("nan"))), (ee.EE_ERR_ARG, dict(eps=float("inf"))), (ee.EE_ERR_ARG, dict(act=4)),
+                      (ee.EE_ERR_ARG, dict(act=-1)), (ee.EE_ERR_ARG, dict(frac_bits=8)), (ee.EE_ERR_ARG, dict(frac_bits=-1)), (ee.EE_ERR_ARG, dict(res_shift=9)),
+                      (ee.EE_ERR_UNSUPPORTED, dict(dtype=2)), (ee.EE_ERR_UNSUPPORTED, dict(dtype=ee.EE_I8, act=3)), (ee.EE_ERR_OVERFLOW, dict(pixels=1 << 25)),
+                      (ee.EE_ERR_OVERFLOW, dict(dtype=ee.EE_I8, pixels=1 << 21))]:
+        d = norm(ee, **bad)
+        assert bytes_of(d) == code, bad
+        assert lib.ee_group_norm(C.byref(d), P, None, None, None, P, None, 0, None) == code, bad
+    d = norm(ee)
+    assert lib.ee_group_norm(C.byref(d), None, None, None, None, P, None, 0, None) == ee.EE_ERR_ARG
+    assert lib.ee_group_norm(C.byref(d), P, None, None, None, None, None, 0, None) == ee.EE_ERR_ARG
+    assert lib.ee_group_norm(C.byref(d), P + 1, None, None, None, P, None, 0, None) == ee.EE_ERR_ARG
+    assert lib.ee_group_norm(C.byref(d), P, P + 2, None, None, P, None, 0, None) == ee.EE_ERR_ARG
+    d = norm(ee, c=8200, groups=1, x_pixel=8200, y_pixel=8200)
+    assert lib.ee_group_norm(C.byref(d), P, None, None, None, P, None, 0, None) == ee.EE_ERR_UNSUPPORTED
+    d = norm(ee, pixels=1 << 20)
+    assert bytes_of(d) == ee.EE_OK
+    assert lib.ee_group_norm(C.byref(d), P, None, None, None, P, None, 0, None) == ee.EE_ERR_ARG
+    assert lib.ee_group_norm(C.byref(d), P, None, None, None, P, P, n.value - 1, None) == ee.EE_ERR_OVERFLOW
+    assert lib.ee_group_norm(C.byref(d), P, None, None, None, P, P + 16, n.value, None) == ee.EE_ERR_ARG
+    assert lib.ee_group_norm(C.byref(norm(ee, b=0)), None, None, None, None, None, None, 0, None) == ee.EE_OK
+    assert lib.ee_group_norm(C.byref(norm(ee, pixels=0)), None, None, None, None, None, None, 0, None) == ee.EE_OK
+
+
+def test_adapter_projection_refuses(ee):
+    lib, n, m = ee.raw(), C.c_int64(-1), C.c_int64(-1)
+    dims = lambda ci=64, co=32, adapters=4, rank=8: ee.AdapterDims(ci, co, adapters, rank)
+    size = lambda d: lib.ee_adapter_bytes(C.byref(d), C.byref(n), C.byref(m))
+    assert size(dims()) == ee.EE_OK and n.value >= 2 * 64 * 32 and m.value >= 2 * 4 * 8 * (64 + 32)
+    assert size(dims(adapters=0, rank=0)) == ee.EE_OK
+    for code, d in [(ee.EE_ERR_ARG, dims(ci=0)), (ee.EE_ERR_ARG, dims(co=0)), (ee.EE_ERR_ARG, dims(adapters=-1)), (ee.EE_ERR_ARG, dims(rank=0)), (ee.EE_ERR_ARG, dims(rank=-1)),
+                    (ee.EE_ERR_OVERFLOW, dims(ci=1 << 19)), (ee.EE_ERR_OVERFLOW, dims(co=1 << 19)), (ee.EE_ERR_OVERFLOW, dims(adapters=1 << 17)), (ee.EE_ERR_OVERFLOW, dims(rank=257))]:
+        assert size(d) == code
+        assert lib.ee_adapter_pack(C.byref(d), P, 1 << 20, None, P, None) == code
+        assert lib.ee_adapter_workspace(C.byref(d), 5, C.byref(n)) == code
+    d = dims()
+    assert lib.ee_adapter_pack(C.byref(d), None, 64, None, P, None) == ee.EE_ERR_ARG
+    assert lib.ee_adapter_pack(C.byref(d), P, 63, None, P, None) == ee.EE_ERR_ARG
+    assert lib.ee_adapter_pack(C.byref(d), P, 64, None, P + 16, None) == ee.EE_ERR_ARG
+    load = lambda i=0, r=8, a=P, lda=64, b=P, ldb=8, pool=P: lib.ee_adapter_load(C.byref(d), i, r, a, lda, b, ldb, 1.0, pool, None)
+    assert [load(i=4), load(i=-1), load(r=9), load(r=-1), load(a=None), load(b=None), load(lda=63), load(ldb=7), load(pool=None), load(pool=P + 128)] == [ee.EE_ERR_ARG] * 10
+    assert lib.ee_adapter_workspace(C.byref(d), -1, C.byref(n)) == ee.EE_ERR_ARG
+    assert lib.ee_adapter_workspace(C.byref(d), (1 << 22) + 1, C.byref(n)) == ee.EE_ERR_OVERFLOW
+    assert lib.ee_adapter_workspace(C.byref(d), 12, C.byref(n)) == ee.EE_OK
+
+    def call(**k):
+        c = dict(packed=P, pool=P, x=P, y=P, ids=P, offsets=None, ldx=64, ldy=32, rows=12, slots=4, per=3, out_f32=0, workspace=P, workspace_bytes=n.value)
+        c.update(k)
+        return lib.ee_adapter_project(C.byref(d), C.byref(ee.AdapterCall(**c)), None)
+    for bad in [dict(packed=None), dict(pool=None), dict(x=None), dict(y=None), dict(ids=None), dict(ldx=63), dict(ldy=31), dict(rows=13), dict(rows=-1), dict(slots=-1), dict(per=-3, slots=-4),
+                dict(workspace=None), dict(workspace=P + 8), dict(x=P + 1), dict(y=P + 2, out_f32=1), dict(ids=P + 2), dict(offsets=P + 1)]:
+        assert call(**bad) == ee.EE_ERR_ARG, bad
+    assert call(workspace_bytes=n.value - 1) == ee.EE_ERR_OVERFLOW
+    assert call(rows=0, slots=0) == ee.EE_OK and call(rows=0, slots=5, per=0) == ee.EE_OK
+    assert lib.ee_adapter_project(C.byref(d), None, None) == ee.EE_ERR_ARG
+
+
+def test_verify_draft_refuses(ee):
+    lib, n = ee.raw(), C.c_int64(-1)
+    assert lib.ee_verify_workspace(3, 4, 1000, C.byref(n)) == ee.EE_OK
+    assert [lib.ee_verify_workspace(-1, 4, 9, C.byref(n)), lib.ee_verify_workspace(1, -1, 9, C.byref(n)), lib.ee_verify_workspace(1, 1, 0, C.byref(n)), lib.ee_verify_workspace(1, 1, 1, None)] == \
+        [ee.EE_ERR_ARG] * 4
+    assert lib.ee_verify_workspace(1, 1, (1 << 30) + 1, C.byref(n)) == ee.EE_ERR_OVERFLOW
+    assert lib.ee_verify_workspace(3, 4, 100000, C.byref(n)) == ee.EE_OK and n.value > 0
+
+    def call(**k):
+        c = dict(draft=P, p=P, q=P, u=P, lengths=P, accepted=P, tokens=P, draft_row=4, u_row=5, p_seq=500000, p_row=100000, q_seq=400000, q_row=100000, b=3, k=4, v=100000, f32=1, workspace=P,
+                 workspace_bytes=n.value)
+        c.update(k)
+        return lib.ee_verify_draft(C.byref(ee.VerifyCall(**c)), None)
+    for bad in [dict(draft=None), dict(p=None), dict(u=None), dict(accepted=None), dict(tokens=None), dict(b=-1), dict(k=-1), dict(v=0), dict(p=P + 2), dict(q=P + 2), dict(q=P + 1, f32=0),
+                dict(draft=P + 1), dict(u=P + 2), dict(lengths=P + 3), dict(accepted=P + 2), dict(tokens=P + 2), dict(workspace=None), dict(workspace=P + 16)]:
+        assert call(**bad) == ee.EE_ERR_ARG, bad
+    assert call(workspace_bytes=n.value - 1) == ee.EE_ERR_OVERFLOW
+    assert call(v=(1 << 30) + 1) == ee.EE_ERR_OVERFLOW and call(b=1 << 24) == ee.EE_ERR_OVERFLOW and call(b=1 << 20, k=1 << 10) == ee.EE_ERR_OVERFLOW
+    assert call(b=0) == ee.EE_OK
+    assert lib.ee_verify_draft(None, None) == ee.EE_ERR_ARG
