@@ -3,7 +3,7 @@
 //   y[m][o] = sum_c x[m][c] W[o][c] + bias[o] + sum_r B_a[o][r] u[m][r],   u[m][r] = scale_a sum_c A_a[r][c] x[m][c],   a: the adapter of row m, or none
 //
 // Two launches.  The first computes u (adapter_shrink_kernel) and the adapter of every row; u is kept as the sum of bf16 numbers (head and remainders:
-// two of them, relative error 2^-18, for bf16 results, three, 2^-26, for float ones), so that the second half of an adapter runs on the matrix cores as well.  The second is the projection, with the adapters as
+// two of them, relative error 2^-18, for bf16 results, three, 2^-26, for float ones), so that the second half of an adapter runs on the matrix cores as well; few rows keep it in float.  The second is the projection, with the adapters as
 // further steps of its reduction: for each adapter among a wavefront's rows, the rows of others read zeros.
 //
 // Weights are laid out once as operands of the matrix instructions: blocks of 32 rows x steps of 16 columns, [lane][8]: lane l holds row l % 32, columns
@@ -24,7 +24,7 @@ struct AdapterKernelArgs {
     const int* ids; const int* offsets; int* row_ids; uint16_t* u;
     const uint16_t* zeros;                                           // 16 readable zero bytes
     int64_t ldx, ldy;
-    int rows, slots, per, ci, co, kp, np, rp, adapters, out_f32, parts;      // parts: bf16 numbers that make up an element of u
+    int rows, slots, per, ci, co, kp, np, rp, ra, adapters, out_f32, parts;      // parts: bf16 numbers that make up an element of u; 0: it is a float
 };
 
 // ---- layouts -----------------------------------------------------------------------------------------------------------------
@@ -61,15 +61,15 @@ __global__ __launch_bounds__(256) void adapter_rows_kernel(const uint16_t* src, 
 
 // ---- first halves ------------------------------------------------------------------------------------------------------------
 // the adapter of a row; -1: none, -2: the row is behind the last slot's
-__device__ __forceinline__ int adapter_of(const AdapterKernelArgs& a, int row)
+__device__ __forceinline__ int adapter_of(const AdapterKernelArgs& a, int row, const int* offsets)
 {
     int slot;
-    if (a.offsets) {
-        if (row < a.offsets[0] || row >= a.offsets[a.slots]) return -2;
+    if (offsets) {
+        if (row < offsets[0] || row >= offsets[a.slots]) return -2;
         int lo = 0, hi = a.slots;                          // offsets[lo] <= row < offsets[hi]
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (a.offsets[mid] <= row) lo = mid;
+            if (offsets[mid] <= row) lo = mid;
             else hi = mid;
         }
         slot = lo;
@@ -78,190 +78,549 @@ __device__ __forceinline__ int adapter_of(const AdapterKernelArgs& a, int row)
     return (unsigned)id < (unsigned)a.adapters ? id : -1;
 }
 
-// u of 16 rows: the wavefronts share the columns of x; 32 rank rows at a time
-__global__ __launch_bounds__(256) void adapter_shrink_kernel(AdapterKernelArgs a)
+enum { OFFSETS_LDS = 2048 };         // up to so many offsets are searched in LDS, more where they lie
+
+// u of ROWS rows (16 or 32: a matrix instruction's), RT x ROWS rows of the adapters' first halves at a time.  Eight wavefronts share the columns of x, 64 at a time, and add up through LDS.
+// 32 rows (many of them): a wavefront loads whole lines of 8 rows and turns them into operands through its own part of LDS; 16 rows: straight from memory, where latency counts.
+// Workgroup `ord` of `ords` takes every ords-th of the different adapters among the rows; neighbours have the same ord, or the ones with nothing to do would leave whole XCDs idle
+// (8,000 rows, 4096 -> 64: 135 us, all of the work on one XCD).
+template <int ROWS, int RT>
+__global__ __launch_bounds__(512) void adapter_shrink_kernel(AdapterKernelArgs a, int blocks, int ords)
 {
-    __shared__ float l_sum[4][32][33];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r0 = blockIdx.x * 32;
-    const int m = r0 + (lane & 31), hi = lane >> 5;
-    const int id = m < a.rows ? adapter_of(a, m) : -2;
-    if (tid < 32 && m < a.rows) a.row_ids[m] = id;
-    const uint16_t* const x = a.x + (int64_t)min(m, a.rows - 1) * a.ldx;
-    const int steps = a.kp / 16;
-    unsigned pending = (unsigned)__ballot(lane < 32 && id >= 0);
-    while (pending) {
-        const int who = __builtin_ctz(pending), ad = __builtin_amdgcn_readlane(id, who);
-        pending &= ~(unsigned)__ballot(lane < 32 && id == ad);
-        const float scale = a.scale[ad];
-        for (int rb = 0; rb < a.rp; rb += 32) {
-            const uint16_t* const w = a.a + ((int64_t)ad * (a.rp / 32) + rb / 32) * steps * 512 + lane * 8;
-            v16f acc = {};
-            for (int s = wave; s < steps; s += 4) {
-                const int col = s * 16 + hi * 8;
-                const v4i xv = col < a.ci ? *(const v4i*)(x + col) : v4i{0, 0, 0, 0};
-                const v4i wv = *(const v4i*)(w + (int64_t)s * 512);
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, wv), __builtin_bit_cast(v8bf, xv), acc, 0, 0, 0);
-            }
+    constexpr int NW = 8, KB = 512 / ROWS, GU = 64 / KB, XL = ROWS == 32 ? 4 : GU;       // KB: columns of a matrix instruction, GU: of them in 64, XL: loads of x a lane makes for them
+    typedef typename std::conditional<ROWS == 32, v16f, v4f>::type acc_t;
+    constexpr int SUM = NW * ROWS * (ROWS + 1) * 4, TURN = ROWS == 32 ? NW * 4096 : 0;
+    __shared__ __attribute__((aligned(16))) unsigned char l_buf[SUM > TURN ? SUM : TURN];
+    __shared__ int l_id[ROWS];
+    __shared__ int l_off[OFFSETS_LDS];
+    float (*const l_sum)[ROWS][ROWS + 1] = (float (*)[ROWS][ROWS + 1])l_buf;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), frow = lane & (ROWS - 1), kq = lane / ROWS;
+    const int ord = blockIdx.x / blocks, block = blockIdx.x - ord * blocks, r0 = block * ROWS, rank0 = blockIdx.y * RT * ROWS;
+    const bool in_lds = a.offsets && a.slots < OFFSETS_LDS;
+    if (in_lds) {
+        for (int i = tid; i <= a.slots; i += 512) l_off[i] = a.offsets[i];
+        __syncthreads();
+    }
+    if (tid < ROWS) {
+        const int m = r0 + tid, id = m < a.rows ? adapter_of(a, m, in_lds ? l_off : a.offsets) : -2;
+        l_id[tid] = id;
+        if (m < a.rows && ord == 0 && blockIdx.y == 0) a.row_ids[m] = id;
+    }
+    __syncthreads();
+    const int id = l_id[frow];
+    const int steps16 = a.kp / 16, chunks = a.kp / 64;
+    // 32 rows: load j is of rows 8 j + lane / 8, 16 bytes each; in LDS piece c of row r is at c ^ (r / 2 & 7): 16 rows in 16 different quads of banks
+    const uint16_t* x[XL];
+    int xcol[XL];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) l_sum[wave][lane & 31][8 * (e >> 2) + 4 * hi + (e & 3)] = acc[e];
+    for (int j = 0; j < XL; ++j) {
+        const int row = ROWS == 32 ? 8 * j + (lane >> 3) : frow;
+        xcol[j] = ROWS == 32 ? (lane & 7) * 8 : j * KB + kq * 8;
+        x[j] = a.x + (int64_t)min(r0 + row, a.rows - 1) * a.ldx + xcol[j];
+    }
+    unsigned char* const turn = l_buf + wave * 4096;
+    unsigned pending = (unsigned)__ballot(lane < ROWS && id >= 0);
+    for (int k = 0; pending; ++k) {
+        const int ad = __builtin_amdgcn_readlane(id, __builtin_ctz(pending));
+        pending &= ~(unsigned)__ballot(lane < ROWS && id == ad);
+        if (k % ords != ord) continue;
+        // operands: 32 rank rows x 16 columns are 64 pieces, columns 8 (piece / 32) .., row piece % 32
+        const uint16_t* w[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int r = min(rank0 + t * ROWS, a.ra - ROWS);
+            w[t] = a.a + ((int64_t)ad * (a.ra / 32) + r / 32) * steps16 * 512 + (ROWS == 32 ? lane * 8 : (kq >> 1) * 512 + ((kq & 1) * 32 + (r & 16) + frow) * 8);
+        }
+        const float scale = a.scale[ad];
+        acc_t acc[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[t] = acc_t{};
+        v4i xv[2][XL], wv[2][RT][GU];
+        auto load = [&](auto buf, int c) {
+            constexpr int B = decltype(buf)::value;
+#pragma unroll
+            for (int j = 0; j < XL; ++j) xv[B][j] = c < chunks && c * 64 + xcol[j] < a.ci ? *(const v4i*)(x[j] + c * 64) : v4i{0, 0, 0, 0};
+#pragma unroll
+            for (int u = 0; u < GU; ++u)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) wv[B][t][u] = *(const v4i*)(w[t] + (int64_t)(min(c, chunks - 1) * 64 + u * KB) / 16 * 512);
+        };
+        auto multiply = [&](auto buf) {
+            constexpr int B = decltype(buf)::value;
+            v4i xo[GU];
+            if constexpr (ROWS == 32) {
+#pragma unroll
+                for (int j = 0; j < XL; ++j) {
+                    const int row = 8 * j + (lane >> 3);
+                    *(v4i*)(turn + row * 128 + (((lane & 7) ^ (row >> 1 & 7)) << 4)) = xv[B][j];
+                }
+#pragma unroll
+                for (int u = 0; u < GU; ++u) xo[u] = *(const v4i*)(turn + frow * 128 + (((2 * u + kq) ^ (frow >> 1 & 7)) << 4));
+            } else
+#pragma unroll
+                for (int u = 0; u < GU; ++u) xo[u] = xv[B][u];
+#pragma unroll
+            for (int u = 0; u < GU; ++u)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    if constexpr (ROWS == 32) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, wv[B][t][u]), __builtin_bit_cast(v8bf, xo[u]), acc[t], 0, 0, 0);
+                    else acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, wv[B][t][u]), __builtin_bit_cast(v8bf, xo[u]), acc[t], 0, 0, 0);
+                }
+        };
+        load(std::integral_constant<int, 0>{}, wave);
+        for (int c = wave; c < chunks; c += 2 * NW) {
+            load(std::integral_constant<int, 1>{}, c + NW);
+            multiply(std::integral_constant<int, 0>{});
+            load(std::integral_constant<int, 0>{}, c + 2 * NW);
+            multiply(std::integral_constant<int, 1>{});                          // past the end: zeros
+        }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            if (rank0 + t * ROWS >= a.rp) break;
+            __syncthreads();                                                     // the sums lie over the operands
+#pragma unroll
+            for (int e = 0; e < (ROWS == 32 ? 16 : 4); ++e) l_sum[wave][frow][ROWS == 32 ? 8 * (e >> 2) + 4 * kq + (e & 3) : 4 * kq + e] = acc[t][e];
             __syncthreads();
-            for (int i = tid; i < 1024; i += 256) {
-                const int row = i >> 5, r = i & 31;
-                if (__shfl(id, row) == ad) {
-                    float v = scale * (l_sum[0][row][r] + l_sum[1][row][r] + l_sum[2][row][r] + l_sum[3][row][r]);
-                    uint16_t* const u = a.u + (int64_t)(r0 + row) * a.parts * a.rp + rb + r;
-                    for (int k = 0; k < a.parts; ++k) {
-                        const __bf16 h = (__bf16)v;
-                        u[k * a.rp] = __builtin_bit_cast(uint16_t, h);
-                        v -= (float)h;
+            for (int i = tid; i < ROWS * ROWS; i += 512) {
+                const int row = i / ROWS, r = i % ROWS;
+                if (l_id[row] == ad && rank0 + t * ROWS + r < a.rp) {
+                    float v = 0.f;
+#pragma unroll
+                    for (int q = 0; q < NW; ++q) v += l_sum[q][row][r];
+                    v *= scale;
+                    if (a.parts == 0) ((float*)a.u)[(int64_t)(r0 + row) * a.rp + rank0 + t * ROWS + r] = v;
+                    else {
+                        uint16_t* const u = a.u + (int64_t)(r0 + row) * a.parts * a.rp + rank0 + t * ROWS + r;
+                        for (int p = 0; p < a.parts; ++p) {
+                            const __bf16 h = (__bf16)v;
+                            u[p * a.rp] = __builtin_bit_cast(uint16_t, h);
+                            v -= (float)h;
+                        }
                     }
                 }
             }
-            __syncthreads();
         }
+        __syncthreads();
     }
 }
 
-// ---- the projection ------------------------------------------------------------------------------------------------------------
-// WM x WN wavefronts, each with MB x NB blocks of 32 rows x 32 outputs.  Rows of x go through LDS, 64 columns at a time, a ring of three;
-// weights straight into registers, eight steps ahead.
-template <int MB, int NB, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void adapter_project_kernel(AdapterKernelArgs a, int gn)
+// ---- the projection, few rows --------------------------------------------------------------------------------------------------
+// A workgroup has 16 outputs and up to 16 MT rows; its eight wavefronts share the reduction, 64 columns at a time, and the adapters, and add up through LDS.  Nothing is staged: a weight is
+// used once.  Reading W is what it is for.
+template <int MT>
+__global__ __launch_bounds__(512) void adapter_rows_project_kernel(AdapterKernelArgs a, int gn)
 {
-    constexpr int NT = 64 * WM * WN, BM = 32 * MB * WM, COPIES = BM * 8 / NT, WR = 8;
-    static_assert(COPIES * NT == BM * 8);
-    __shared__ __attribute__((aligned(16))) unsigned char lds[3 * BM * 128];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hi = lane >> 5, frow = lane & 31;
-    const int wm = wave % WM, wn = wave / WM;
-    const int mt = blockIdx.x / gn, nt = blockIdx.x % gn, m0 = mt * BM, n0 = (nt * WN + wn) * NB;      // n0: first block of 32 outputs
-    const unsigned lds0 = lds_addr(lds);
-    const int iters = a.kp / 64, steps = iters * 4, blocks = a.np / 32;
-    // copies: LDS position q = 8 row + pos holds chunk pos ^ (row & 7) of the row
-    const uint16_t* src[COPIES];
-    int chunk[COPIES];
+    constexpr int NW = 8;
+    __shared__ float l_sum[NW][16 * MT][17];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), frow = lane & 15, kq = lane >> 4;
+    const int nb = blockIdx.x % gn, m0 = blockIdx.x / gn * 16 * MT;          // nb: block of 16 outputs
+    const int steps16 = a.kp / 16, chunks = a.kp / 64;
+    const int piece = ((kq & 1) * 32 + (nb & 1) * 16 + frow) * 8;
+    const uint16_t* const w = a.w + (int64_t)(nb >> 1) * steps16 * 512 + (kq >> 1) * 512 + piece;
+    const uint16_t* x[MT];
 #pragma unroll
-    for (int j = 0; j < COPIES; ++j) {
-        const int q = tid + NT * j, row = q >> 3;
-        chunk[j] = (q & 7) ^ (row & 7);
-        src[j] = a.x + (int64_t)min(m0 + row, a.rows - 1) * a.ldx;
-    }
-    auto copy = [&](int it) {
-        const int slot = it % 3;
+    for (int i = 0; i < MT; ++i) x[i] = a.x + (int64_t)min(m0 + 16 * i + frow, a.rows - 1) * a.ldx + kq * 8;
+    v4f acc[MT];
 #pragma unroll
-        for (int j = 0; j < COPIES; ++j) {
-            const int col = it * 64 + chunk[j] * 8;
-            dma16(lds0 + (unsigned)(slot * BM * 128 + (NT * j + 64 * wave) * 16), it < iters && col < a.ci ? src[j] + col : a.zeros);
+    for (int i = 0; i < MT; ++i) acc[i] = v4f{};
+    v4i wv[2][2], xv[2][2][MT];
+    auto load = [&](auto buf, int c) {
+        constexpr int B = decltype(buf)::value;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int col = c * 64 + u * 32;
+            wv[B][u] = *(const v4i*)(w + (int64_t)(min(c, chunks - 1) * 4 + 2 * u) * 512);
+            const bool in = c < chunks && col + kq * 8 < a.ci;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) xv[B][u][i] = in ? *(const v4i*)(x[i] + col) : v4i{0, 0, 0, 0};
         }
     };
-    const uint16_t* w[NB];
+    auto multiply = [&](auto buf) {
+        constexpr int B = decltype(buf)::value;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) w[n] = a.w + (int64_t)min(n0 + n, blocks - 1) * steps * 512 + lane * 8;
-    auto weight = [&](int n, int s) { return *(const v4i*)(w[n] + (int64_t)min(s, steps - 1) * 512); };
-    v4i wr[WR][NB];
-    copy(0);
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int s = 0; s < WR; ++s)
+            for (int i = 0; i < MT; ++i)
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, wv[B][u]), __builtin_bit_cast(v8bf, xv[B][u][i]), acc[i], 0, 0, 0);
+    };
+    // outputs a thread finishes: row tid / 16 + 32 j, output tid % 16 of the block; their adapters in vector arithmetic, 16 of the rank at a time, the first of them loaded up front
+    constexpr int J = MT == 4 ? 2 : 1;
+    const int o = nb * 16 + (tid & 15);
+    int id[J];
+    const v4f* u[J];
+    const uint16_t* b[J];
+    v4f uv[J][4];
+    v4i bv[J][2];
 #pragma unroll
-        for (int n = 0; n < NB; ++n) wr[s][n] = weight(n, s);
-    copy(1);
+    for (int j = 0; j < J; ++j) {
+        const int row = (tid >> 4) + 32 * j, m = m0 + row;
+        id[j] = row < 16 * MT && m < a.rows ? a.row_ids ? a.row_ids[m] : -1 : -2;
+        u[j] = (const v4f*)((const float*)a.u + (int64_t)m * a.rp);
+        b[j] = a.b + (((int64_t)id[j] * (a.np / 32) + (nb >> 1)) * (a.rp / 16) * 64 + (nb & 1) * 16 + (tid & 15)) * 8;
+    }
+    auto load_adapter = [&](int j, int r) {
+        if (id[j] < 0) return;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) uv[j][e] = u[j][r / 4 + e];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) bv[j][e] = *(const v4i*)(b[j] + (r / 16 * 64 + e * 32) * 8);
+    };
+    load(std::integral_constant<int, 0>{}, wave);
+#pragma unroll
+    for (int j = 0; j < J; ++j) load_adapter(j, 0);
+    const float bias = a.bias[min(o, a.np - 1)];
+    for (int c = wave; c < chunks; c += 2 * NW) {
+        load(std::integral_constant<int, 1>{}, c + NW);
+        multiply(std::integral_constant<int, 0>{});
+        load(std::integral_constant<int, 0>{}, c + 2 * NW);
+        multiply(std::integral_constant<int, 1>{});
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) l_sum[wave][16 * i + frow][4 * kq + e] = acc[i][e];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int row = (tid >> 4) + 32 * j;
+        if (id[j] == -2 || o >= a.co) continue;
+        float v = bias;
+#pragma unroll
+        for (int q = 0; q < NW; ++q) v += l_sum[q][row][tid & 15];
+        if (id[j] >= 0)
+            for (int r = 0; r < a.rp; r += 16) {
+                if (r) load_adapter(j, r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t two = (uint32_t)bv[j][e >> 2][e & 3];
+                    v = fmaf(uv[j][e >> 1][2 * e & 3], __uint_as_float(two << 16), v);
+                    v = fmaf(uv[j][e >> 1][(2 * e & 3) + 1], __uint_as_float(two & 0xFFFF0000u), v);
+                }
+            }
+        const int m = m0 + row;
+        if (a.out_f32) ((float*)a.y)[m * a.ldy + o] = v;
+        else ((uint16_t*)a.y)[m * a.ldy + o] = __builtin_bit_cast(uint16_t, (__bf16)v);
+    }
+}
+
+// ---- the projection, many rows ---------------------------------------------------------------------------------------------------
+// KG groups of WM x WN wavefronts share the reduction, a slab of 32 columns of x and W each at a time; a wavefront has MB x NB blocks of 32 rows x 32 outputs.  Slabs go through LDS, a ring
+// of stages per group filled by asynchronous copies: those of step t + RING - 1 start, and those of t + 1 are waited for, at the barrier in front of step t, so that the operands of a step's
+// first instructions are read before its barrier.
+// The adapters are further slabs: for each different one among the tile's rows, the parts of u (rows of others: zeros) and its second half.
+template <int MB, int NB, int WM, int WN, int KG, int RING, bool F32>
+__global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(AdapterKernelArgs a, int gm, int gn)
+{
+    constexpr int NW = WM * WN, NT = 64 * NW * KG, BM = 32 * MB * WM, BN = 32 * NB * WN, STAGE = (BM + BN) * 64, XU = BM / 16 / NW, WU = BN / 16 / NW;      // XU, WU: KiB a wavefront copies per stage
+    static_assert(XU * 16 * NW == BM && WU * 16 * NW == BN && BM <= 256 && BM % 64 == 0);
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    int* const l_list = (int*)(lds + KG * RING * STAGE);   // different adapters of the rows, their number
+    int* const l_ids = l_list + BM + 4;                    // adapter of every row
+    const int tid = threadIdx.x, lane = tid & 63, wave_all = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wave_all / NW, wave = wave_all % NW, hi = lane >> 5, frow = lane & 31;
+    const int wm = wave % WM, wn = wave / WM;
+    // tiles in groups of four along the rows, in a group the rows first; each XCD an eighth of them, one behind the other: what its tiles read at a time fits its L2
+    const int unit = xcd_unit(blockIdx.x, gm * gn);
+    if (unit < 0) return;
+    const int group = unit / (4 * gn), in = unit - group * 4 * gn, tall = min(4, gm - group * 4), nt = in / tall, mt = group * 4 + in - nt * tall;
+    const int m0 = mt * BM, nb0 = nt * WN * NB, n0 = nb0 + wn * NB;      // nb0, n0: the tile's, the wavefront's first block of 32 outputs
+    const unsigned lds0 = lds_addr(lds) + (unsigned)(kg * RING * STAGE);
+    unsigned char* const ring = lds + kg * RING * STAGE;
+    const int slabs = a.kp / 32, blocks = a.np / 32, kx = a.parts * a.rp, per = (kx + 31) / 32, rs = a.rp / 16;      // per: slabs an adapter takes
+    for (int r = tid; r < BM; r += NT) l_ids[r] = m0 + r < a.rows ? a.row_ids ? a.row_ids[m0 + r] : -1 : -2;
+    // LDS of a stage: rows of 64 bytes, position p of row r holds chunk p ^ (r / 4 & 3) (16 rows are in 16 different quads of banks) | operands of W, a KiB per block and step of 16
+    const unsigned char* const xt = (const unsigned char*)(a.x + (int64_t)m0 * a.ldx);
+    unsigned from[XU];                                     // bytes from there: the host bounds 256 rows by 2 GiB
+#pragma unroll
+    for (int j = 0; j < XU; ++j) {
+        const int row = 16 * (j * NW + wave) + (lane >> 2);
+        from[j] = (unsigned)min(row, a.rows - 1 - m0) * (unsigned)(2 * a.ldx) + (unsigned)((lane & 3) ^ (row >> 2 & 3)) * 16u;
+    }
+    const unsigned char* w[WU];                            // uniform
+#pragma unroll
+    for (int j = 0; j < WU; ++j) {
+        const int u = j * NW + wave;
+        w[j] = (const unsigned char*)a.w + ((int64_t)min(nb0 + u / 2, blocks - 1) * slabs * 2 + u % 2) * 1024;
+    }
+    const unsigned wlane = (unsigned)lane * 16u;
+    // where step `it` goes in the ring, and the slab that is this group's
+    auto stage = [&](int it) { return (unsigned)(it % RING * STAGE); };
+    auto slab = [&](int it) { return it * KG + kg; };
+    // piece j of a step: XU of x, then WU of W.  Slabs of whole 32 columns only
+    auto piece = [&](int it, auto j_tag) {
+        constexpr int J = decltype(j_tag)::value;
+        const unsigned to = lds0 + stage(it) + (unsigned)(wave * 1024);
+        if constexpr (J < XU) dma16(to + (unsigned)(NW * J * 1024), xt + (int64_t)slab(it) * 64, from[J]);
+        else dma16(to + (unsigned)(BM * 64 + NW * (J - XU) * 1024), w[J - XU] + (int64_t)slab(it) * 2048, wlane);
+    };
+    auto copy = [&](int it) {
+        if ((slab(it) + 1) * 32 <= a.ci) {
+            static_for<XU + WU>([&](auto j) { piece(it, j); });
+            return;
+        }
+        const unsigned to = lds0 + stage(it) + (unsigned)(wave * 1024);
+#pragma unroll
+        for (int j = 0; j < XU; ++j) {                     // the last columns, where they are no whole 32: zeros behind them
+            const int row = 16 * (j * NW + wave) + (lane >> 2), col = slab(it) * 32 + ((lane & 3) ^ (row >> 2 & 3)) * 8;
+            dma16(to + (unsigned)(NW * j * 1024), col < a.ci ? (const void*)(xt + (int64_t)slab(it) * 64 + from[j]) : a.zeros);
+        }
+        static_for<WU>([&](auto j) { piece(it, std::integral_constant<int, decltype(j)::value + XU>{}); });
+    };
+    // slab e of adapter ad; ad < 0: past the end, zeros
+    auto copy_adapter = [&](int it, int ad, int e) {
+        const unsigned to = lds0 + stage(it) + (unsigned)(wave * 1024);
+#pragma unroll
+        for (int j = 0; j < XU; ++j) {
+            const int row = 16 * (j * NW + wave) + (lane >> 2), k = e * 32 + ((lane & 3) ^ (row >> 2 & 3)) * 8;
+            dma16(to + (unsigned)(NW * j * 1024), ad >= 0 && l_ids[row] == ad && k < kx ? a.u + (int64_t)(m0 + row) * kx + k : a.zeros);
+        }
+#pragma unroll
+        for (int j = 0; j < WU; ++j) {
+            const int u = j * NW + wave;
+            const unsigned char* const b = (const unsigned char*)a.b + (((int64_t)ad * blocks + min(nb0 + u / 2, blocks - 1)) * rs + (e * 2 + u % 2) % rs) * 1024;
+            dma16(to + (unsigned)(BM * 64 + NW * j * 1024), ad >= 0 ? b : (const unsigned char*)a.w, wlane);
+        }
+    };
+    constexpr int EARLY = KG <= 2 ? 2 / KG : 0;            // steps that are slabs of x for certain: kp is a multiple of 64
+    static_for<EARLY>([&](auto k) { copy(decltype(k)::value); });
+    __syncthreads();
+    if (wave_all == 0) {
+        int mine[BM / 64], n = 0;
+#pragma unroll
+        for (int i = 0; i < BM / 64; ++i) mine[i] = l_ids[64 * i + lane];
+        for (;;) {
+            int ad = -1;
+#pragma unroll
+            for (int i = 0; i < BM / 64; ++i) {
+                const unsigned long long b = __ballot(mine[i] >= 0);
+                if (ad < 0 && b) ad = __builtin_amdgcn_readlane(mine[i], __builtin_ctzll(b));
+            }
+            if (ad < 0) break;
+#pragma unroll
+            for (int i = 0; i < BM / 64; ++i) mine[i] = mine[i] == ad ? -1 : mine[i];
+            if (lane == 0) l_list[n] = ad;
+            ++n;
+        }
+        if (lane == 0) l_list[BM] = n;
+    }
+    lds_barrier();
+    const int total = slabs + __builtin_amdgcn_readfirstlane(l_list[BM]) * per, iters = (total + KG - 1) / KG;
+    auto copy_any = [&](int it) {
+        const int s = slab(it), e = s - slabs;
+        if (e < 0) copy(it);
+        else copy_adapter(it, s < total ? __builtin_amdgcn_readfirstlane(l_list[e / per]) : -1, s < total ? e % per : 0);
+    };
+#pragma unroll
+    for (int k = EARLY; k < RING - 1; ++k) copy_any(k);
+    unsigned at[2];                                        // x, step of 16
+#pragma unroll
+    for (int k = 0; k < 2; ++k) at[k] = (unsigned)((wm * MB * 32 + frow) * 64 + (((2 * k + hi) ^ (frow >> 2 & 3)) << 4));
+    const unsigned wat = (unsigned)(BM * 64 + wn * NB * 2048) + wlane;
+    // operands are read two steps of 16 columns before they are used, into four sets in turn: a read takes as long as four to eight matrix instructions when all wavefronts read
+    v4i xv[4][MB], wv[4][NB];
+    auto read = [&](auto set, int it, auto step, auto n_tag) {           // operand n_tag of a step, in the order they are used: w 0, x 0, the rest of w, the rest of x
+        constexpr int S = decltype(set)::value, K = decltype(step)::value, N = decltype(n_tag)::value, X = N == 1 ? 0 : N > NB ? N - NB : -1, W = N == 0 ? 0 : N - 1;
+        const unsigned char* const base = ring + stage(it);
+        if constexpr (X >= 0) xv[S][X] = *(const v4i*)(base + at[K] + X * 2048);
+        else wv[S][W] = *(const v4i*)(base + wat + (W * 2 + K) * 1024);
+    };
     v16f acc[MB][NB];
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
         for (int n = 0; n < NB; ++n) acc[i][n] = v16f{};
-    auto iteration = [&](auto half, int it) {
-        constexpr int H = decltype(half)::value * 4;
-        // copies newer than this iteration's: one iteration's, and 4 NB weights of each of the last two iterations at least
-        wait_all_then_barrier<COPIES + 4 * NB>();
-        copy(it + 2);
-        const unsigned char* const base = lds + (it % 3) * BM * 128 + (wm * MB * 32 + frow) * 128;
-        static_for<4>([&](auto ks_tag) {
-            constexpr int KS = decltype(ks_tag)::value;
-            v4i xv[MB];
+    // the MB x NB instructions of a step; behind instruction k: f(k)
+    auto multiply = [&](auto set, auto&& f) {
+        constexpr int S = decltype(set)::value;
+        static_for<MB * NB>([&](auto k_tag) {
+            constexpr int K = decltype(k_tag)::value, I = K / NB, N = K % NB;
+            acc[I][N] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, wv[S][N]), __builtin_bit_cast(v8bf, xv[S][I]), acc[I][N], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            f(k_tag);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    // things 0 .. count - 1, as evenly behind the first SLOTS instructions as whole numbers allow
+    auto spread = [&](auto k_tag, auto count, auto slots, auto&& g) {
+        constexpr int K = decltype(k_tag)::value, COUNT = decltype(count)::value, SLOTS = decltype(slots)::value, LO = K < SLOTS ? K * COUNT / SLOTS : COUNT, HI = K < SLOTS ? (K + 1) * COUNT / SLOTS : COUNT;
+        static_for<HI - LO>([&](auto d) { g(std::integral_constant<int, LO + decltype(d)::value>{}); });
+    };
+    using operands = std::integral_constant<int, MB + NB>;
+    using pieces = std::integral_constant<int, XU + WU>;
+    using every = std::integral_constant<int, MB * NB>;
+    using front = std::integral_constant<int, (MB * NB + 1) / 2>;
+    // Step `it` of parity P; the copies go out between matrix instructions: all of a workgroup's at once would hold up the instructions behind them
+    auto iteration = [&](auto parity, int it, auto fast) {
+        constexpr int P = decltype(parity)::value;
+        constexpr bool FAST = decltype(fast)::value;
+        wait_copies_then_barrier<(RING - 3) * (XU + WU)>();      // step it + 1 is there, step it - 1 has been read by all
+        if constexpr (!FAST) copy_any(it + RING - 1);
+        static_for<2>([&](auto step) {
+            constexpr int K = decltype(step)::value;
+            multiply(std::integral_constant<int, 2 * P + K>{}, [&](auto k) {
+                spread(k, operands{}, front{}, [&](auto n) { read(std::integral_constant<int, 2 * (1 - P) + K>{}, it + 1, step, n); });
+                if constexpr (FAST && K == 0) spread(k, pieces{}, every{}, [&](auto j) { piece(it + RING - 1, j); });
+            });
+        });
+    };
+    wait_copies_then_barrier<(RING - 2) * (XU + WU)>();
+    static_for<2>([&](auto k) { static_for<MB + NB>([&](auto n) { read(k, 0, k, n); }); });
+    int it = 0;
+    const int full = min(a.ci / 32 / KG, iters) - (RING - 1);   // steps that copy whole slabs of x
+    for (; it + 2 <= full; it += 2) static_for<2>([&](auto p) { iteration(p, it + decltype(p)::value, std::true_type{}); });
+    for (; it < iters; it += 2)                            // where the number is odd one step more, of zeros
+        static_for<2>([&](auto p) { iteration(p, it + decltype(p)::value, std::false_type{}); });
+
+    // ---- results: a lane has row frow of a block, outputs 8 q + 4 hi + 0..3; through LDS, a wavefront's 32 rows of 32 NB outputs at a time, to whole pieces of 16 bytes ----
+    constexpr int ES = F32 ? 4 : 2, VEC = 16 / ES, PIECES = 32 * NB / VEC, PITCH = 32 * NB * ES + 16;
+    constexpr int SUMS = KG > 1 ? (KG - 1) * NW * MB * NB * 4096 : 0;                        // the results' part of LDS is behind the sums'
+    static_assert(SUMS + NW * 32 * PITCH <= KG * RING * STAGE);
+    unsigned char* const mine = lds + SUMS + wave * 32 * PITCH;
+    const int first = n0 * 32;
+    const bool whole = ((uintptr_t)a.y & 15) == 0 && a.ldy % VEC == 0;
+    v4f bias[NB][4];
 #pragma unroll
-            for (int i = 0; i < MB; ++i) xv[i] = *(const v4i*)(base + i * 4096 + (((2 * KS + hi) ^ (frow & 7)) << 4));
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) bias[n][q] = first < a.np && first + n * 32 < a.np ? *(const v4f*)(a.bias + first + n * 32 + 8 * q + 4 * hi) : v4f{0.f, 0.f, 0.f, 0.f};
+    wait_all_then_barrier<0>();                            // every wavefront is done with the ring, its copies are too
+    if constexpr (KG > 1) {                                // the groups' sums, through LDS, to the first one
+        static_assert((KG - 1) * NW * MB * NB * 4096 <= KG * RING * STAGE);
+        v4f* const l_part = (v4f*)lds + (size_t)wave * MB * NB * 256 + lane;                  // [group][wavefront][block][quad][lane]
+        if (kg > 0)
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
-                    acc[i][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, wr[H + KS][n]), __builtin_bit_cast(v8bf, xv[i]), acc[i][n], 0, 0, 0);
 #pragma unroll
-            for (int n = 0; n < NB; ++n) wr[H + KS][n] = weight(n, it * 4 + KS + WR);
-        });
-    };
-    int it = 0;
-    for (; it + 2 <= iters; it += 2) {
-        iteration(std::integral_constant<int, 0>{}, it);
-        iteration(std::integral_constant<int, 1>{}, it + 1);
+                    for (int q = 0; q < 4; ++q) {
+                        v4f v;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = acc[i][n][4 * q + e];
+                        l_part[((kg - 1) * NW * MB * NB + i * NB + n) * 256 + q * 64] = v;
+                    }
+        lds_barrier();
+        if (kg > 0) return;
+#pragma unroll
+        for (int g = 0; g < KG - 1; ++g)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const v4f v = l_part[(g * NW * MB * NB + i * NB + n) * 256 + q * 64];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][n][4 * q + e] += v[e];
+                    }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    if (it < iters) iteration(std::integral_constant<int, 0>{}, it);
-
-    // ---- adapters: further reductions (one per part of u) over the rank for each adapter among the rows ----------------
-    int id[MB];
-    unsigned pending[MB];
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
-        const int m = m0 + (wm * MB + i) * 32 + frow;
-        id[i] = m < a.rows ? a.row_ids[m] : -2;
-        pending[i] = (unsigned)__ballot(lane < 32 && id[i] >= 0);
-    }
-    for (;;) {
-        int ad = -1;
-#pragma unroll
-        for (int i = 0; i < MB; ++i)
-            if (ad < 0 && pending[i]) ad = __builtin_amdgcn_readlane(id[i], __builtin_ctz(pending[i]));
-        if (ad < 0) break;
-        const uint16_t* const wb = a.b + (int64_t)ad * blocks * (a.rp / 16) * 512 + lane * 8;
-        for (int r = 0; r < a.rp; r += 16) {
-            v4i bv[NB];
-#pragma unroll
-            for (int n = 0; n < NB; ++n) bv[n] = *(const v4i*)(wb + ((int64_t)min(n0 + n, blocks - 1) * (a.rp / 16) + r / 16) * 512);
-#pragma unroll
-            for (int i = 0; i < MB; ++i) {
-                const uint16_t* const u = a.u + (int64_t)(m0 + (wm * MB + i) * 32 + frow) * a.parts * a.rp + r + hi * 8;
-                for (int part = 0; part < a.parts; ++part) {
-                    const v4i uv = id[i] == ad ? *(const v4i*)(u + part * a.rp) : v4i{0, 0, 0, 0};
-#pragma unroll
-                    for (int n = 0; n < NB; ++n)
-                        acc[i][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, bv[n]), __builtin_bit_cast(v8bf, uv), acc[i][n], 0, 0, 0);
-                }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < MB; ++i) pending[i] &= ~(unsigned)__ballot(lane < 32 && id[i] == ad);
-    }
-
-    // ---- results: lane: row frow of a block, outputs 8 q + 4 hi + 0..3 of a block ---------------------------------------------
-#pragma unroll
-    for (int i = 0; i < MB; ++i) {
-        const int m = m0 + (wm * MB + i) * 32 + frow;
-        if (m >= a.rows || id[i] == -2) continue;
+        const int r0 = (wm * MB + i) * 32;
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < 4; ++q) {
+                v4f v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int o = (n0 + n) * 32 + 8 * q + 4 * hi + e;
-                    if (o >= a.co) continue;
-                    const float v = acc[i][n][4 * q + e] + a.bias[o];
-                    if (a.out_f32) ((float*)a.y)[m * a.ldy + o] = v;
-                    else ((uint16_t*)a.y)[m * a.ldy + o] = __builtin_bit_cast(uint16_t, (__bf16)v);
-                }
+                for (int e = 0; e < 4; ++e) v[e] = acc[i][n][4 * q + e] + bias[n][q][e];
+                unsigned char* const cell = mine + frow * PITCH + (n * 32 + 8 * q + 4 * hi) * ES;
+                if constexpr (F32) *(v4f*)cell = v;
+                else *(uint2*)cell = uint2{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
+            }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int c = 0; c < 32 * PIECES / 64; ++c) {
+            const int q = 64 * c + lane, row = q / PIECES, o = first + q % PIECES * VEC;
+            const v4i v = *(const v4i*)(mine + row * PITCH + q % PIECES * 16);
+            if (l_ids[r0 + row] == -2 || o >= a.co) continue;
+            unsigned char* const y = (unsigned char*)a.y + ((int64_t)(m0 + r0 + row) * a.ldy + o) * ES;
+            if (whole && o + VEC <= a.co) *(v4i*)y = v;
+            else
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (o + e < a.co) {
+                        if constexpr (F32) ((int*)y)[e] = v[e];
+                        else ((uint16_t*)y)[e] = (uint16_t)((unsigned)v[e >> 1] >> (16 * (e & 1)));
+                    }
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
 struct AdapterSizes {       // in bytes; everything a multiple of 256
-    int64_t kp, np, rp, w, bias, a, b, scale;
+    int64_t kp, np, rp, ra, w, bias, a, b, scale;          // rp, ra: the rank as a reduction's length, as rows
     explicit AdapterSizes(const AdapterDims& d)
     {
-        kp = up(d.ci, 64); np = up(d.co, 32); rp = up(std::max(d.rank, 1), 32);
+        kp = up(d.ci, 64); np = up(d.co, 32); rp = up(std::max(d.rank, 1), 16); ra = up(rp, 32);
         w = 2 * np * kp; bias = up(4 * np, 256);
-        a = 2 * rp * kp * d.adapters; b = 2 * np * rp * d.adapters; scale = up(4ll * d.adapters, 256);
+        a = 2 * ra * kp * d.adapters; b = 2 * np * rp * d.adapters; scale = up(4ll * d.adapters, 256);
     }
 };
+
+hipError_t launch_shrink(const AdapterKernelArgs& k, hipStream_t s)
+{
+    // few rows: 16 at a time, and a workgroup for every adapter that may be among them; many rows of one slot each: two may be, of packed ones any number
+    const int rows = k.rows <= 1024 ? 16 : 32, blocks = (k.rows + rows - 1) / rows, most = k.offsets ? 4 : k.per >= rows ? 2 : rows;
+    int ords = 1;
+    while (ords < (rows == 16 ? 16 : most) && 2 * ords * blocks <= 2048) ords *= 2;
+    auto go = [&](auto kernel, int rt) {
+        EE_LAUNCH(kernel, dim3((unsigned)(blocks * ords), (unsigned)((k.rp + rt * rows - 1) / (rt * rows))), dim3(512), 0, s, k, blocks, ords);
+        return hipGetLastError();
+    };
+    if (rows == 16) return k.rp <= 16 ? go(adapter_shrink_kernel<16, 1>, 1) : k.rp <= 32 ? go(adapter_shrink_kernel<16, 2>, 2) : go(adapter_shrink_kernel<16, 4>, 4);
+    return k.rp <= 32 ? go(adapter_shrink_kernel<32, 1>, 1) : go(adapter_shrink_kernel<32, 2>, 2);
+}
+
+// Whether the kernel for few rows is the one: up to 32 rows, and where a short reduction over few outputs leaves the tiles little to do or the adapters that may be among a tile's rows lengthen
+// it by a quarter.  Both launches, us, this kernel / 64 x 64 tiles, eight adapters of rank 16: 4096 -> 4096 16 rows 16.2 / 23.4, 32 rows 19.8 / 24.6, 64 rows 27.8 / 27.1, 128 rows 45 / 28;
+// 2048 -> 8192 32 rows 18.0 / 18.1, 48 rows 25.0 / 18.7; 1024 -> 256 64 rows 11.0 / 13.2, 512 rows 11.4 / 13.4; 2048 -> 1000 64 rows 15.9 / 16.2 (24 adapters: 17 / 28), 256 rows 17.5 / 16.3
+bool few_rows(const AdapterKernelArgs& k)
+{
+    if (k.rows <= 32) return true;
+    const int different = std::min(std::min(k.adapters, k.slots), 64 / std::max(1, k.rows / k.slots) + 1);
+    const bool short_tiles = k.ci <= 1024 || different * (2 * k.rp + 31) / 32 * 4 >= k.kp / 32;
+    return short_tiles && (int64_t)((k.rows + 63) / 64) * ((k.co + 15) / 16) <= 256;
+}
+
+hipError_t launch_few_rows(const AdapterKernelArgs& k, hipStream_t s)
+{
+    const int gn = (k.co + 15) / 16;
+    auto go = [&](auto kernel, int mt) {
+        EE_LAUNCH(kernel, dim3((unsigned)((k.rows + 16 * mt - 1) / (16 * mt) * gn)), dim3(512), 0, s, k, gn);
+        return hipGetLastError();
+    };
+    return k.rows <= 16 ? go(adapter_rows_project_kernel<1>, 1) : k.rows <= 32 ? go(adapter_rows_project_kernel<2>, 2) : go(adapter_rows_project_kernel<4>, 4);
+}
+
+template <int MB, int NB, int WM, int WN, int KG, int RING, bool F32>
+hipError_t launch_tiles(const AdapterKernelArgs& k, hipStream_t s)
+{
+    constexpr int BM = 32 * MB * WM, BN = 32 * NB * WN;
+    constexpr unsigned LDS = KG * RING * (BM + BN) * 64 + 8 * BM + 16;
+    static const hipError_t granted = hipFuncSetAttribute(reinterpret_cast<const void*>(&adapter_project_kernel<MB, NB, WM, WN, KG, RING, F32>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    if (granted != hipSuccess) return granted;
+    const int gm = (k.rows + BM - 1) / BM, gn = (k.co + BN - 1) / BN;
+    EE_LAUNCH((adapter_project_kernel<MB, NB, WM, WN, KG, RING, F32>), dim3(xcd_grid((long long)gm * gn)), dim3(64 * WM * WN * KG), LDS, s, k, gm, gn);
+    return hipGetLastError();
+}
+
+template <int MB, int NB, int WM, int WN, int KG, int RING>
+hipError_t launch_form(const AdapterKernelArgs& k, hipStream_t s) { return k.out_f32 ? launch_tiles<MB, NB, WM, WN, KG, RING, true>(k, s) : launch_tiles<MB, NB, WM, WN, KG, RING, false>(k, s); }
+
+hipError_t launch_many_rows(const AdapterKernelArgs& k, hipStream_t s)
+{
+    auto tiles = [&](int bm, int bn) { return (int64_t)((k.rows + bm - 1) / bm) * ((k.co + bn - 1) / bn); };
+    // The largest tile that gives every CU one: while there are fewer tiles than CUs the reduction is a chain, and smaller tiles with two groups of wavefronts make it shorter.  4096 -> 4096, us
+    // with one adapter: 256 rows 64 x 64 tiles 26, 64 x 128 32, 128 x 128 37; 512 rows 42, 34, 39; 1024 rows 75, 60, 45
+    if (tiles(64, 64) <= 256) return launch_form<1, 1, 2, 2, 2, 8>(k, s);
+    if (tiles(64, 128) <= 256) return launch_form<1, 2, 2, 2, 2, 6>(k, s);
+    if (tiles(128, 128) <= 256) return launch_form<2, 2, 2, 2, 2, 4>(k, s);
+    // More: in units of a round of 256 tiles of 256 x 256, a round of 256 tiles of 128 x 128 takes 0.37.  4096 -> 4096: 2048 rows 88 and 81 us, 3000 rows 102 and 116, 8192 rows 218 and 266
+    return (double)((tiles(256, 256) + 255) / 256) < 0.37 * (double)((tiles(128, 128) + 255) / 256) ? launch_form<4, 2, 2, 4, 1, 4>(k, s) : launch_form<2, 2, 2, 2, 1, 4>(k, s);
+}
 
 hipError_t pack(const void* src, int64_t ld, int rows, int cols, void* dst, int64_t blocks, int64_t steps, hipStream_t s)
 {
@@ -291,7 +650,7 @@ hipError_t launch_adapter_load(const AdapterDims& d, int i, int rank, const void
 {
     const AdapterSizes z(d);
     char* const p = (char*)pool;
-    hipError_t e = pack(a, lda, rank, d.ci, p + z.a / std::max(d.adapters, 1) * i, z.rp / 32, z.kp / 16, s);
+    hipError_t e = pack(a, lda, rank, d.ci, p + z.a / d.adapters * i, z.ra / 32, z.kp / 16, s);
     if (e == hipSuccess) e = pack(b, ldb, d.co, rank, p + z.a + z.b / d.adapters * i, z.np / 32, z.rp / 16, s);
     if (e != hipSuccess) return e;
     EE_LAUNCH(adapter_scale_kernel, dim3(1), dim3(1), 0, s, (float*)(p + z.a + z.b) + i, scale);
@@ -306,25 +665,18 @@ hipError_t launch_adapter_project(const AdapterDims& d, const AdapterCall& c, hi
     k.w = (const uint16_t*)c.packed; k.bias = (const float*)((const char*)c.packed + z.w); k.zeros = (const uint16_t*)((const char*)c.packed + z.w + z.bias);
     k.a = (const uint16_t*)c.pool; k.b = (const uint16_t*)((const char*)c.pool + z.a); k.scale = (const float*)((const char*)c.pool + z.a + z.b);
     k.ids = c.ids; k.offsets = c.offsets; k.rows = c.rows; k.slots = c.slots; k.per = c.per;
-    k.ci = d.ci; k.co = d.co; k.kp = (int)z.kp; k.np = (int)z.np; k.rp = (int)z.rp; k.adapters = d.adapters; k.parts = c.out_f32 ? 3 : 2;
+    k.ci = d.ci; k.co = d.co; k.kp = (int)z.kp; k.np = (int)z.np; k.rp = (int)z.rp; k.ra = (int)z.ra; k.adapters = d.adapters; k.parts = few_rows(k) ? 0 : c.out_f32 ? 3 : 2;
     char* ws = (char*)c.workspace;
     k.u = (uint16_t*)ws; ws += up(6ll * c.rows * z.rp, 256);
     k.row_ids = (int*)ws; ws += up(4ll * c.rows, 256);
-    if (((uintptr_t)c.x & 15) || c.ldx % 8 || d.ci % 8) {
+    if (((uintptr_t)c.x & 15) || c.ldx % 8 || d.ci % 8 || c.ldx > 1 << 21) {
         EE_LAUNCH(adapter_rows_kernel, dim3((unsigned)(((int64_t)c.rows * z.kp + 255) / 256)), dim3(256), 0, s, k.x, k.ldx, c.rows, d.ci, (uint16_t*)ws, k.kp);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         k.x = (const uint16_t*)ws; k.ldx = k.kp; k.ci = k.kp;
     }
-    EE_LAUNCH(adapter_shrink_kernel, dim3((c.rows + 31) / 32), dim3(256), 0, s, k);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (c.rows <= 64) {
-        const int gn = (int)(z.np + 127) / 128;
-        EE_LAUNCH((adapter_project_kernel<1, 1, 1, 4>), dim3((unsigned)((c.rows + 31) / 32 * gn)), dim3(256), 0, s, k, gn);
-    } else {
-        const int gn = (int)(z.np + 127) / 128;
-        EE_LAUNCH((adapter_project_kernel<2, 2, 2, 2>), dim3((unsigned)((c.rows + 127) / 128 * gn)), dim3(256), 0, s, k, gn);
-    }
-    return hipGetLastError();
+    if (d.adapters == 0 && !c.offsets) k.row_ids = nullptr;           // every row has none
+    else if (const hipError_t e = launch_shrink(k, s); e != hipSuccess) return e;
+    return few_rows(k) ? launch_few_rows(k, s) : launch_many_rows(k, s);
 }
 
 }  // namespace ee
