@@ -17,9 +17,18 @@ int check_norm(const ee_norm_desc* d, NormArgs& a)
     if (d->act < EE_ACT_NONE || d->act > EE_ACT_SILU) return EE_ERR_ARG;
     if (d->dtype == EE_I8 && d->act == EE_ACT_SILU) return EE_ERR_UNSUPPORTED;
     if ((int64_t)d->pixels * d->c >= 1ll << 31 || (d->dtype == EE_I8 && (int64_t)d->pixels * (d->c / d->groups) >= 1 << 24)) return EE_ERR_OVERFLOW;
+    const int64_t es = d->dtype == EE_I8 ? 1 : 2;
+    if (d->pixels > 1) {
+        for (const int64_t stride : {d->x_pixel, d->res_pixel, d->y_pixel})
+            if (stride < 0) return EE_ERR_ARG;
+        if (d->y_pixel < d->c) return EE_ERR_ARG;
+        for (const int64_t stride : {d->x_pixel, d->res_pixel, d->y_pixel})
+            if (stride >= 1 << 20 || ((d->pixels + 1024) * stride + d->c) * es >= 1ll << 31) return EE_ERR_OVERFLOW;
+    }
     a = NormArgs{};
     a.dtype = d->dtype; a.act = d->act; a.b = d->b; a.pixels = d->pixels; a.c = d->c; a.groups = d->groups; a.frac_bits = d->frac_bits; a.res_shift = d->res_shift; a.eps = d->eps;
     a.x_sample = d->x_sample; a.x_pixel = d->x_pixel; a.res_sample = d->res_sample; a.res_pixel = d->res_pixel; a.y_sample = d->y_sample; a.y_pixel = d->y_pixel;
+    if (a.pixels == 1) a.x_pixel = a.res_pixel = a.y_pixel = a.c;
     return EE_OK;
 }
 

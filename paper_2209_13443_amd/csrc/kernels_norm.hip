@@ -5,12 +5,14 @@
 //   int8  S1 = sum x, S2 = sum x^2 (exact integers), d = n x - S1, m_c = weight_c 2^f / (n sqrt((n S2 - S1^2) / n^2 + eps)),
 //         y = clamp(floor(d m_c + (bias_c 2^f + 1/2) + res 2^rs), lo, hi) in 64-bit floats: d is exact, so a constant group gives its bias on
 //         every machine and the results are whole numbers that do not depend on the order of a sum
-// Statistics of bf16: every thread has the mean and the sum of squared differences from it of its own values, in registers, and the pairs are merged
+// Statistics of bf16: every lane adds up the differences of its values from one of them, and their squares, has from those its own mean and sum of squared differences from it, and such
+// pairs are merged
 // (n = na + nb, delta = mb - ma: mean = ma + delta nb / n, M2 = M2a + M2b + delta^2 na nb / n), so that a mean far from zero costs nothing.
 //
 // Bound by memory.  A workgroup has a window of whole groups (columns of 16 bytes, a power of two of them) and some pixels of one sample; a lane has one
 // column and every NT / columns-th pixel.  Where the window of a whole sample fits a workgroup's registers it is one launch that reads x once; else two:
 // statistics of chunks of pixels, then every workgroup of the second launch merges the chunks of its sample and writes its part (x is read again).
+// int8 results: in float arithmetic, and again in 64 bits where that is too near to a whole number to say on which side (about one vector of 16 in a thousand).
 #include <algorithm>
 #include <type_traits>
 
@@ -23,11 +25,11 @@ namespace {
 struct NormKernelArgs {
     const void* x; const void* res; void* y;
     const float* weight; const float* bias;
-    void* part;                      // split form: [sample][chunk][group] pairs
+    void* part;                      // two launches: [sample][chunk][group] pairs
     int64_t x_sample, x_pixel, r_sample, r_pixel, y_sample, y_pixel;      // strides in elements
     int pixels, c, groups, cpg;
     int cw, wlog;                    // channels of a window (whole groups), log2 of its columns (idle ones included)
-    int windows, chunks, chunk_pixels;
+    int windows, chunks, chunk_pixels, units;                             // units: workgroups with work
     float eps;
     double out_scale, res_scale;     // int8: 2^frac_bits, 2^res_shift
     int act, lo, hi;
@@ -42,6 +44,7 @@ __device__ __forceinline__ void merge(Moments& a, float nb, float mb, float m2b)
     a.m2 += fmaf(d * d, a.n * w, m2b);
     a.n = n;
 }
+// int8: the sum and the sum of squares
 struct Sums { int s1; long long s2; };
 
 template <int ES> struct elem;
@@ -65,313 +68,430 @@ struct Pack {       // VEC elements of a pixel, as loaded
     }
 };
 
-__device__ __forceinline__ float activate(float v, int act)      // a NaN stays one
+// The pixels of a window and chunk as a lane sees them: `step` pixels on from its first, by buffer instructions, which drop what lies behind the last pixel (loads read zeros there).  A lane
+// without channels is behind it everywhere.  The host bounds what a sample spans by 2 GiB
+template <int ES, int VEC>
+struct View {
+    typedef typename Pack<ES, VEC>::raw raw;
+    __amdgpu_buffer_rsrc_t r;
+    unsigned off;
+    int pitch;
+    __device__ __forceinline__ View(const void* base, int64_t pixel, int pixels, int channels, bool live, int row, int col)
+    {
+        pitch = (int)pixel * ES;
+        r = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, pixels ? (pixels - 1) * pitch + channels * ES : 0, 0x00020000);
+        off = live ? (unsigned)(row * pitch + col * VEC * ES) : 0x80000000u;
+    }
+    __device__ __forceinline__ raw load(int step) const
+    {
+        if constexpr (VEC > 1) return __builtin_bit_cast(raw, __builtin_amdgcn_raw_buffer_load_b128(r, off + (unsigned)(step * pitch), 0, 0));
+        else if constexpr (ES == 2) return __builtin_bit_cast(raw, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, off + (unsigned)(step * pitch), 0, 0));
+        else return __builtin_bit_cast(raw, (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, off + (unsigned)(step * pitch), 0, 0));
+    }
+    __device__ __forceinline__ void store(raw v, int step) const
+    {
+        typedef unsigned v4u __attribute__((ext_vector_type(4)));
+        if constexpr (VEC > 1) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, v), r, off + (unsigned)(step * pitch), 0, 0);
+        else if constexpr (ES == 2) __builtin_amdgcn_raw_buffer_store_b16(v, r, off + (unsigned)(step * pitch), 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b8((uint8_t)v, r, off + (unsigned)(step * pitch), 0, 0);
+    }
+};
+
+template <int ACT>
+__device__ __forceinline__ float activate(float v)               // a NaN stays one
 {
-    if (act == EE_ACT_RELU) return v < 0.f ? 0.f : v;
-    if (act == EE_ACT_RELU6) return v < 0.f ? 0.f : v > 6.f ? 6.f : v;
-    if (act == EE_ACT_SILU) return v * __builtin_amdgcn_rcpf(1.f + __expf(-v));
+    if constexpr (ACT == EE_ACT_RELU) return v < 0.f ? 0.f : v;
+    if constexpr (ACT == EE_ACT_RELU6) return v < 0.f ? 0.f : v > 6.f ? 6.f : v;
+    if constexpr (ACT == EE_ACT_SILU) return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * v));
     return v;
 }
 
-// MODE 0: the whole sample's window in one workgroup, 1: statistics of a chunk, 2: merge the chunks of the sample, write one chunk.
+// the pair of lanes that differ in bit `off` of their number: both get the merged value, from the same order
+__device__ __forceinline__ void merge_pair(Moments& m, float nb, float mb, float qb, bool second)
+{
+    Moments lo = m;
+    if (second) { lo = {nb, mb, qb}; merge(lo, m.n, m.mean, m.m2); }
+    else merge(lo, nb, mb, qb);
+    m = lo;
+}
+__device__ __forceinline__ void merge_lanes(Moments& m, int off, int lane) { merge_pair(m, __shfl_xor(m.n, off), __shfl_xor(m.mean, off), __shfl_xor(m.m2, off), lane & off); }
+__device__ __forceinline__ void merge_lanes(Sums& s, int off, int)
+{
+    s.s1 += __shfl_xor(s.s1, off);
+    s.s2 += __shfl_xor(s.s2, off);
+}
+
+// FORM 0: the whole sample's window in one workgroup, 1: statistics of a chunk, 2: merge the chunks of the sample, write one chunk.
 // GPV: partial results per column (each of VEC / GPV channels of one group)
-template <int ES, int VEC, int GPV, int NT, int NV, int MODE>
+template <int ES, int VEC, int GPV, int NT, int NV, int FORM>
 __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
 {
     using P = Pack<ES, VEC>;
     using T = typename elem<ES>::type;
-    constexpr int SUB = VEC / GPV;
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    const int tid = threadIdx.x, cols = 1 << a.wlog, col = tid & (cols - 1), row = tid >> a.wlog, rows = NT >> a.wlog;
-    int u = blockIdx.x;
-    const int win = u % a.windows; u /= a.windows;
-    const int chunk = u % a.chunks, b = u / a.chunks;
-    const int c0 = win * a.cw, cw = min(a.cw, a.c - c0), wgroups = cw / a.cpg;
-    const bool live = col * VEC < cw;
-    const int p0 = chunk * a.chunk_pixels, p1 = min(a.pixels, p0 + a.chunk_pixels);
-    const T* const x = (const T*)a.x + b * a.x_sample + c0 + col * VEC;
-
-    // ---- LDS: per-lane partials of the reduction | per group | per channel --------------------------------------------
-    const int slices = NT / max(64, cols);
-    float* const l_n = (float*)lds;                                  // [slices][cols] counts (bf16)
-    unsigned char* const l_part = lds + (ES == 2 ? 4 * slices * cols : 0);
-    // pairs [slices][cols][GPV]
+    using raw = typename P::raw;
+    typedef typename std::conditional<ES == 2, Moments, Sums>::type stat_t;
     typedef typename std::conditional<ES == 2, float2, Sums>::type pair_t;
-    pair_t* const part = (pair_t*)l_part;
-    float2* const l_group = (float2*)(l_part + sizeof(pair_t) * slices * cols * GPV);      // bf16: mean, 1 / sqrt(var + eps); int8: S1 and factor as doubles
-    double2* const l_group_d = (double2*)l_group;
-    const double n_all = (double)a.pixels * a.cpg;
+    constexpr int SUB = VEC / GPV, LOG_NT = NT == 256 ? 8 : 10;
+    static_assert(NT == 256 || NT == 1024);
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int u = xcd_unit(blockIdx.x, a.units);
+    if (u < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, cols = 1 << a.wlog, col = tid & (cols - 1), row = tid >> a.wlog, rows = NT >> a.wlog;
+    const int win = u % a.windows, uc = u / a.windows, chunk = uc % a.chunks, b = uc / a.chunks;
+    const int c0 = win * a.cw, cw = min(a.cw, a.c - c0), wgroups = cw / a.cpg;
+    const int p0 = chunk * a.chunk_pixels, end = min(a.pixels, p0 + a.chunk_pixels);
+    const bool live = col * VEC < cw;
+    const int p1 = live ? end : p0;                                  // a lane without channels has no pixels
+    const View<ES, VEC> x((const T*)a.x + b * a.x_sample + p0 * a.x_pixel + c0, a.x_pixel, end - p0, cw, live, row, col);
 
-    typename P::raw data[NV];
-    auto load = [&](int base) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int p = base + row + i * rows;
-            if (live && p < p1) data[i] = *(const typename P::raw*)(x + p * a.x_pixel);
+    const int slices = NT / max(64, cols);
+    float* const l_n = (float*)lds;                                                                  // bf16: values of the lanes of a slice and column
+    pair_t* const l_part = (pair_t*)(lds + (ES == 2 ? 4 * slices * cols : 0));                       // [slice][column][GPV]
+    unsigned char* const l_group = (unsigned char*)(l_part + slices * cols * GPV);                   // per group: bf16 mean and 1 / deviation; int8 S1 and 1 / (n deviation)
+    const double n_all = (double)a.pixels * a.cpg;
+    auto settle = [&](int g, const stat_t& s) {
+        if constexpr (ES == 2) ((float2*)l_group)[g] = float2{s.mean, rsqrtf(s.m2 / (float)n_all + a.eps)};
+        else {
+            const long long n = (long long)a.pixels * a.cpg;
+            const double var = (double)(n * s.s2 - (long long)s.s1 * s.s1) / (n_all * n_all);
+            ((double2*)l_group)[g] = double2{(double)s.s1, 1.0 / (n_all * sqrt(var + (double)a.eps))};
         }
     };
-    auto have = [&](int base) { return !live || base + row >= p1 ? 0 : min(NV, (p1 - base - row - 1) / rows + 1); };
-
-    // ---- statistics ---------------------------------------------------------------------------------------------------
-    if constexpr (MODE != 2) {
-        Moments mo[GPV];
-        Sums su[GPV];
-#pragma unroll
-        for (int j = 0; j < GPV; ++j) { mo[j] = {0.f, 0.f, 0.f}; su[j] = {0, 0}; }
-        for (int base = p0; base < p1; base += NV * rows) {
-            load(base);
-            const int cnt = have(base);
-            if constexpr (ES == 2) {
-                const float nb = (float)(cnt * SUB);
-#pragma unroll
-                for (int j = 0; j < GPV; ++j) {
-                    float s = 0.f, q = 0.f;
-#pragma unroll
-                    for (int i = 0; i < NV; ++i)
-                        if (i < cnt)
-#pragma unroll
-                            for (int e = 0; e < SUB; ++e) s += P::f(data[i], j * SUB + e);
-                    const float m = s / fmaxf(nb, 1.f);                  // a division: equal values have exactly their value as mean
-#pragma unroll
-                    for (int i = 0; i < NV; ++i)
-                        if (i < cnt)
-#pragma unroll
-                            for (int e = 0; e < SUB; ++e) {
-                                const float d = P::f(data[i], j * SUB + e) - m;
-                                q = fmaf(d, d, q);
-                            }
-                    if (cnt) merge(mo[j], nb, m, q);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < GPV; ++j) {
-                    int s = 0, q = 0;
-#pragma unroll
-                    for (int i = 0; i < NV; ++i)
-                        if (i < cnt)
-#pragma unroll
-                            for (int e = 0; e < SUB; ++e) {
-                                const int v = P::i(data[i], j * SUB + e);
-                                s += v;
-                                q += v * v;
-                            }
-                    su[j].s1 += s;
-                    su[j].s2 += q;
-                }
-            }
-        }
-        // lanes of a wavefront with the same column, then slices of the workgroup through LDS
-        const int lane = tid & 63;
-#pragma unroll 1
-        for (int off = cols; off < 64; off <<= 1) {
-            if constexpr (ES == 2) {
-                const float nb = __shfl_xor(mo[0].n, off);
-#pragma unroll
-                for (int j = 0; j < GPV; ++j) {
-                    const float mb = __shfl_xor(mo[j].mean, off), qb = __shfl_xor(mo[j].m2, off);
-                    // both lanes of a pair merge in the same order
-                    Moments lo = mo[j];
-                    if (lane & off) { lo = {nb, mb, qb}; merge(lo, mo[j].n, mo[j].mean, mo[j].m2); }
-                    else merge(lo, nb, mb, qb);
-                    mo[j] = lo;
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < GPV; ++j) {
-                    su[j].s1 += __shfl_xor(su[j].s1, off);
-                    su[j].s2 += __shfl_xor(su[j].s2, off);
-                }
-            }
-        }
-        if (cols >= 64 || lane < cols) {
-            const int slice = cols >= 64 ? row : tid >> 6, at = slice * cols + col;
-            if constexpr (ES == 2) {
-                l_n[at] = mo[0].n;
-#pragma unroll
-                for (int j = 0; j < GPV; ++j) part[at * GPV + j] = float2{mo[j].mean, mo[j].m2};
-            } else {
-#pragma unroll
-                for (int j = 0; j < GPV; ++j) part[at * GPV + j] = su[j];
-            }
-        }
-        __syncthreads();
-        // a group is cpg / SUB neighbouring partials of every slice: 2^sl lanes of a wavefront take them in turn
-        const int per = a.cpg / SUB, entries = per * slices;
+    // every group of the window, 2^sl lanes each that take its `entries` in turn: s = sum of get(group, entry); then f(group, s) in one lane
+    auto per_group = [&](int entries, auto&& get, auto&& f) {
         int sl = 0;
         while (sl < 6 && (1 << sl) < entries) ++sl;
         const int lanes = 1 << sl, sub = tid & (lanes - 1);
         for (int g0 = 0; g0 < wgroups; g0 += NT >> sl) {
             const int g = g0 + (tid >> sl);
-            Moments m = {0.f, 0.f, 0.f};
-            Sums s = {0, 0};
+            stat_t s{};
             if (g < wgroups)
-                for (int e = sub; e < entries; e += lanes) {
-                    const int slice = e / per, slot = g * per + e - slice * per;           // slot: partial of the window
-                    const int at = slice * cols + slot / GPV;
-                    if constexpr (ES == 2) {
-                        const float2 v = part[at * GPV + slot % GPV];
-                        merge(m, l_n[at], v.x, v.y);
-                    } else {
-                        const Sums v = part[at * GPV + slot % GPV];
-                        s.s1 += v.s1;
-                        s.s2 += v.s2;
-                    }
-                }
+                for (int e = sub; e < entries; e += lanes) get(g, e, s);
 #pragma unroll 1
-            for (int off = 1; off < lanes; off <<= 1) {
-                if constexpr (ES == 2) {
-                    const float nb = __shfl_xor(m.n, off), mb = __shfl_xor(m.mean, off), qb = __shfl_xor(m.m2, off);
-                    Moments lo = m;
-                    if (sub & off) { lo = {nb, mb, qb}; merge(lo, m.n, m.mean, m.m2); }
-                    else merge(lo, nb, mb, qb);
-                    m = lo;
-                } else {
-                    s.s1 += __shfl_xor(s.s1, off);
-                    s.s2 += __shfl_xor(s.s2, off);
-                }
-            }
-            if (g < wgroups && sub == 0) {
-                if constexpr (MODE == 1) {
-                    const size_t at = ((size_t)b * a.chunks + chunk) * a.groups + c0 / a.cpg + g;
-                    if constexpr (ES == 2) ((float2*)a.part)[at] = float2{m.mean, m.m2};
-                    else ((Sums*)a.part)[at] = s;
-                } else if constexpr (ES == 2) l_group[g] = float2{m.mean, rsqrtf(m.m2 / (float)n_all + a.eps)};
-                else {
-                    const long long n = (long long)a.pixels * a.cpg;
-                    const double var = (double)(n * s.s2 - (long long)s.s1 * s.s1) / (n_all * n_all);
-                    l_group_d[g] = double2{(double)s.s1, 1.0 / (n_all * sqrt(var + (double)a.eps))};
-                }
-            }
+            for (int off = 1; off < lanes; off <<= 1) merge_lanes(s, off, lane);
+            if (g < wgroups && sub == 0) f(g, s);
         }
-    }
-    if constexpr (MODE == 1) return;
-    if constexpr (MODE == 2) {
-        int sl = 0;
-        while (sl < 6 && (1 << sl) < a.chunks) ++sl;
-        const int lanes = 1 << sl, sub = tid & (lanes - 1);
-        for (int g0 = 0; g0 < wgroups; g0 += NT >> sl) {
-            const int g = g0 + (tid >> sl);
-            Moments m = {0.f, 0.f, 0.f};
-            long long s1 = 0, s2 = 0;
-            if (g < wgroups)
-                for (int k = sub; k < a.chunks; k += lanes) {
-                    const size_t at = ((size_t)b * a.chunks + k) * a.groups + c0 / a.cpg + g;
-                    if constexpr (ES == 2) {
-                        const float2 v = ((const float2*)a.part)[at];
-                        merge(m, (float)(min(a.chunk_pixels, a.pixels - k * a.chunk_pixels)) * a.cpg, v.x, v.y);
-                    } else {
-                        const Sums v = ((const Sums*)a.part)[at];
-                        s1 += v.s1;
-                        s2 += v.s2;
-                    }
-                }
-#pragma unroll 1
-            for (int off = 1; off < lanes; off <<= 1) {
-                if constexpr (ES == 2) {
-                    const float nb = __shfl_xor(m.n, off), mb = __shfl_xor(m.mean, off), qb = __shfl_xor(m.m2, off);
-                    Moments lo = m;
-                    if (sub & off) { lo = {nb, mb, qb}; merge(lo, m.n, m.mean, m.m2); }
-                    else merge(lo, nb, mb, qb);
-                    m = lo;
-                } else {
-                    s1 += __shfl_xor(s1, off);
-                    s2 += __shfl_xor(s2, off);
-                }
-            }
-            if (g < wgroups && sub == 0) {
-                if constexpr (ES == 2) l_group[g] = float2{m.mean, rsqrtf(m.m2 / (float)n_all + a.eps)};
-                else {
-                    const long long n = (long long)a.pixels * a.cpg;
-                    const double var = (double)(n * s2 - s1 * s1) / (n_all * n_all);
-                    l_group_d[g] = double2{(double)s1, 1.0 / (n_all * sqrt(var + (double)a.eps))};
-                }
-            }
-        }
-    }
-    __syncthreads();
-    if (!live) return;
+    };
 
-    // ---- normalise, residual, activation --------------------------------------------------------------------------------
-    const T* const res = a.res ? (const T*)a.res + b * a.r_sample + c0 + col * VEC : nullptr;
-    T* const y = (T*)a.y + b * a.y_sample + c0 + col * VEC;
-    if constexpr (ES == 2) {
-        float mean[VEC], scale[VEC], shift[VEC];
+    constexpr int TV = NV;                                            // vectors a lane holds of x (two launches: of two sets)
+    raw data[TV];
+    const bool has_res = FORM != 1 && a.res;
+    const View<ES, VEC> res((const T*)a.res + b * a.r_sample + p0 * a.r_pixel + c0, a.r_pixel, has_res ? end - p0 : 0, cw, live, row, col);
+#pragma unroll
+    for (int i = 0; i < TV; ++i) data[i] = x.load(i * rows);         // pixels are counted from p0 from here on
+    const int count = end - p0, mine = p1 - p0;
+    // the lane's channels' factors, loaded with the first pixels
+    constexpr bool AFFINE = FORM != 1 && (ES == 2 || VEC == 1);
+    float weight[AFFINE ? VEC : 1], bias[AFFINE ? VEC : 1];
+    if constexpr (AFFINE)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            const int c = c0 + col * VEC + e;
-            const float2 g = l_group[(col * VEC + e) / a.cpg];
-            mean[e] = g.x;
-            scale[e] = g.y * (a.weight ? a.weight[c] : 1.f);
-            shift[e] = a.bias ? a.bias[c] : 0.f;
+            const int c = min(c0 + col * VEC + e, a.c - 1);
+            weight[e] = a.weight ? a.weight[c] : 1.f;
+            bias[e] = a.bias ? a.bias[c] : 0.f;
         }
-        for (int base = p0; base < p1; base += NV * rows) {
-            if constexpr (MODE == 2) load(base);
+    // what was unpacked from a vector is not kept for the next time
+    auto forget = [&](raw& v) {
+        if constexpr (VEC > 1) asm volatile("" : "+v"(v));
+    };
+
+    if constexpr (FORM != 2) {
+        // bf16: sums of x - pivot and of its square, the pivot a value of the lane's own (its first): as far from the mean as values of the group are.  mean and m2 hold them until all are added.
+        // Vectors behind the lane's last pixel read as what adds nothing: pivots, int8 zeros
+        stat_t st[GPV] = {};
+        float pivot[ES == 2 ? GPV : 1];
+        const int values = row < mine ? ((mine - row - 1) >> (LOG_NT - a.wlog)) + 1 : 0;      // vectors of the lane
+        raw fill{};
+        if constexpr (ES == 2) {
+#pragma unroll
+            for (int j = 0; j < GPV; ++j) pivot[j] = values ? P::f(data[0], j * SUB) : 0.f;
+            if constexpr (VEC == 1) fill = values ? data[0] : raw{};
+            else
+#pragma unroll
+                for (int e = 0; e < VEC; e += 2) fill[e >> 1] = (int)(__float_as_uint(pivot[e / SUB]) >> 16 | (__float_as_uint(pivot[(e + 1) / SUB]) & 0xFFFF0000u));
+        }
+        auto add = [&](raw (&v)[NV], int base) {
+            if (base + NV * rows > count)
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (base + i * rows + row >= mine) v[i] = fill;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int p = base + row + i * rows;
-                if (p >= p1) continue;
-                typename P::raw r{};
-                if (res) r = *(const typename P::raw*)(res + p * a.r_pixel);
+#pragma unroll
+                for (int j = 0; j < GPV; ++j) {
+                    if constexpr (ES == 2) {
+#pragma unroll
+                        for (int e = 0; e < SUB; ++e) {
+                            const float d = P::f(v[i], j * SUB + e) - pivot[j];
+                            st[j].mean += d;
+                            st[j].m2 = fmaf(d, d, st[j].m2);
+                        }
+                    } else {
+                        int q = 0;
+                        if constexpr (SUB % 4 == 0)
+#pragma unroll
+                            for (int e = 0; e < SUB / 4; ++e) {
+                                const int w = v[i][j * SUB / 4 + e];
+                                st[j].s1 = __builtin_amdgcn_sdot4(w, 0x01010101, st[j].s1, false);
+                                q = __builtin_amdgcn_sdot4(w, w, q, false);
+                            }
+                        else
+#pragma unroll
+                            for (int e = 0; e < SUB; ++e) {
+                                const int x1 = P::i(v[i], j * SUB + e);
+                                st[j].s1 += x1;
+                                q += x1 * x1;
+                            }
+                        st[j].s2 += q;
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        if constexpr (FORM == 0) add(data, 0);
+        else {                                                       // the next pixels are on their way while these are added
+            raw d2[NV];
+#pragma unroll 1
+            for (int base = 0; base < count; base += 2 * NV * rows) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) d2[i] = x.load(base + (NV + i) * rows);
+                add(data, base);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) data[i] = x.load(base + (2 * NV + i) * rows);
+                add(d2, base + NV * rows);
+            }
+        }
+        if constexpr (ES == 2) {
+            const float n = (float)values * SUB, inv = __builtin_amdgcn_rcpf(fmaxf(n, 1.f));
+#pragma unroll
+            for (int j = 0; j < GPV; ++j) {
+                const float d = st[j].mean * inv;
+                st[j].n = n;
+                st[j].m2 = fmaxf(fmaf(-d, st[j].mean, st[j].m2), 0.f) + 0.f * st[j].m2;      // not below 0 by rounding; a NaN stays one
+                st[j].mean = pivot[j] + d;
+            }
+        }
+        // lanes of a wavefront with the same column, then slices of the workgroup through LDS
+#pragma unroll 1
+        for (int off = cols; off < 64; off <<= 1) {
+            if constexpr (ES == 2) {
+                const float nb = __shfl_xor(st[0].n, off);
+#pragma unroll
+                for (int j = 0; j < GPV; ++j) merge_pair(st[j], nb, __shfl_xor(st[j].mean, off), __shfl_xor(st[j].m2, off), lane & off);
+            } else
+#pragma unroll
+                for (int j = 0; j < GPV; ++j) merge_lanes(st[j], off, lane);
+        }
+        if (cols >= 64 || lane < cols) {
+            const int slice = cols >= 64 ? row : tid >> 6, at = slice * cols + col;
+            if constexpr (ES == 2) l_n[at] = st[0].n;
+#pragma unroll
+            for (int j = 0; j < GPV; ++j) {
+                if constexpr (ES == 2) l_part[at * GPV + j] = float2{st[j].mean, st[j].m2};
+                else l_part[at * GPV + j] = st[j];
+            }
+        }
+        __syncthreads();
+        const int per = a.cpg / SUB;                                 // a group is so many neighbouring partials of every slice
+        per_group(per * slices,
+                  [&](int g, int e, stat_t& s) {
+                      const int slice = e / per, slot = g * per + e - slice * per, at = slice * cols + slot / GPV;
+                      const pair_t v = l_part[at * GPV + slot % GPV];
+                      if constexpr (ES == 2) merge(s, l_n[at], v.x, v.y);
+                      else { s.s1 += v.s1; s.s2 += v.s2; }
+                  },
+                  [&](int g, const stat_t& s) {
+                      if constexpr (FORM == 1) {
+                          const size_t at = ((size_t)b * a.chunks + chunk) * a.groups + c0 / a.cpg + g;
+                          if constexpr (ES == 2) ((float2*)a.part)[at] = float2{s.mean, s.m2};
+                          else ((Sums*)a.part)[at] = s;
+                      } else settle(g, s);
+                  });
+    }
+    if constexpr (FORM == 1) return;
+    if constexpr (FORM == 2) {
+        per_group(a.chunks,
+                  [&](int g, int k, stat_t& s) {
+                      const size_t at = ((size_t)b * a.chunks + k) * a.groups + c0 / a.cpg + g;
+                      if constexpr (ES == 2) {
+                          const float2 v = ((const float2*)a.part)[at];
+                          merge(s, (float)(min(a.chunk_pixels, a.pixels - k * a.chunk_pixels)) * a.cpg, v.x, v.y);
+                      } else {
+                          const Sums v = ((const Sums*)a.part)[at];
+                          s.s1 += v.s1;
+                          s.s2 += v.s2;
+                      }
+                  },
+                  settle);
+    }
+    __syncthreads();
+
+    // ---- normalise, residual, activation --------------------------------------------------------------------------------
+    const View<ES, VEC> y((const T*)a.y + b * a.y_sample + p0 * a.y_pixel + c0, a.y_pixel, end - p0, cw, live, row, col);
+    // f(x, residual) -> y for every vector of the lane, four at a time, the next four's residuals (FORM 2: and x) on their way
+    auto tiles = [&](auto res_tag, auto&& f) {
+        constexpr bool RES = decltype(res_tag)::value;
+        constexpr int BV = TV < 4 ? TV : 4;
+        raw r[2][BV], d2[BV];
+        auto residuals = [&](raw (&to)[BV], int i0) {
+            if constexpr (RES)
+#pragma unroll
+                for (int i = 0; i < BV; ++i) to[i] = res.load(i0 + i * rows);
+        };
+        auto four = [&](raw* d, raw (&rr)[BV], int i0) {
+#pragma unroll
+            for (int i = 0; i < BV; ++i) {
+                forget(d[i]);
+                y.store(f(d[i], rr[i]), i0 + i * rows);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        residuals(r[0], 0);
+        if constexpr (FORM == 0) {
+#pragma unroll
+            for (int k = 0; k < TV / BV; ++k) {
+                if (k + 1 < TV / BV) residuals(r[(k + 1) & 1], (k + 1) * BV * rows);
+                four(data + k * BV, r[k & 1], k * BV * rows);
+            }
+        } else {
+#pragma unroll 1
+            for (int base = 0; base < count; base += 2 * BV * rows) {
+#pragma unroll
+                for (int i = 0; i < BV; ++i) d2[i] = x.load(base + (BV + i) * rows);
+                residuals(r[1], base + BV * rows);
+                four(data, r[0], base);
+#pragma unroll
+                for (int i = 0; i < BV; ++i) data[i] = x.load(base + (2 * BV + i) * rows);
+                residuals(r[0], base + 2 * BV * rows);
+                four(d2, r[1], base + BV * rows);
+            }
+        }
+    };
+    if constexpr (ES == 2) {
+        float mean[GPV];
+#pragma unroll
+        for (int j = 0; j < GPV; ++j) {
+            const float2 g = ((const float2*)l_group)[min((col * VEC + j * SUB) / a.cpg, wgroups - 1)];
+            mean[j] = g.x;
+#pragma unroll
+            for (int e = 0; e < SUB; ++e) weight[j * SUB + e] *= g.y;
+        }
+        auto run = [&](auto act_tag, auto res_tag) {
+            constexpr int ACT = decltype(act_tag)::value;
+            constexpr bool RES = decltype(res_tag)::value;
+            tiles(res_tag, [&](const raw& d, const raw& r) {
                 float v[VEC];
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    v[e] = fmaf(P::f(data[i], e) - mean[e], scale[e], shift[e]);
-                    if (res) v[e] += P::f(r, e);
-                    v[e] = activate(v[e], a.act);
+                    v[e] = fmaf(P::f(d, e) - mean[e / SUB], weight[e], bias[e]);
+                    if constexpr (RES) v[e] += P::f(r, e);
+                    v[e] = activate<ACT>(v[e]);
                 }
-                if constexpr (VEC == 1) y[p * a.y_pixel] = __builtin_bit_cast(uint16_t, (__bf16)v[0]);
+                if constexpr (VEC == 1) return __builtin_bit_cast(uint16_t, (__bf16)v[0]);
                 else {
                     v4i o;
 #pragma unroll
                     for (int e = 0; e < VEC; e += 2) o[e >> 1] = (int)pack2_bf16(v[e], v[e + 1]);
-                    *(v4i*)(y + p * a.y_pixel) = o;
+                    return o;
                 }
-            }
-        }
+            });
+        };
+        auto with = [&](auto act_tag) {
+            if (has_res) run(act_tag, std::true_type{});
+            else run(act_tag, std::false_type{});
+        };
+        if (a.act == EE_ACT_NONE) with(std::integral_constant<int, EE_ACT_NONE>{});
+        else if (a.act == EE_ACT_RELU) with(std::integral_constant<int, EE_ACT_RELU>{});
+        else if (a.act == EE_ACT_RELU6) with(std::integral_constant<int, EE_ACT_RELU6>{});
+        else with(std::integral_constant<int, EE_ACT_SILU>{});
     } else {
-        for (int base = p0; base < p1; base += NV * rows) {
-            if constexpr (MODE == 2) load(base);
-            int q[NV][VEC];
+        auto group_of = [&](int e) { return ((const double2*)l_group)[min((col * VEC + e) / a.cpg, wgroups - 1)]; };
+        // per channel, in 64 bits: factor, offset
+        auto channel = [&](float w, float bi, double2 g) { return double2{(double)w * a.out_scale * g.y, (double)bi * a.out_scale + 0.5}; };
+        auto in_64 = [&](int v, int r, double s1, double2 c) {       // the definition
+            double t = fma(n_all * v - s1, c.x, c.y);
+            if (has_res) t += r * a.res_scale;
+            return (int)fmin(fmax(floor(t), (double)a.lo), (double)a.hi);
+        };
+        if constexpr (VEC == 1) {
+            const double2 c = channel(weight[0], bias[0], group_of(0));
+            const double s1 = group_of(0).x;
+            if (has_res) tiles(std::true_type{}, [&](const raw& d, const raw& r) { return (int8_t)in_64(d, r, s1, c); });
+            else tiles(std::false_type{}, [&](const raw& d, const raw&) { return (int8_t)in_64(d, 0, s1, c); });
+        } else {
+            // in float, of bytes + 128 (one instruction turns a byte without sign into a float), the result moved up by 128 as well: t = x f + h + (r + 128) rs
+            // the factors of a channel, once per workgroup
+            float2* const l_channel = (float2*)(l_group + 16 * (a.cw / a.cpg));
+            const float rs = has_res ? (float)a.res_scale : 0.f;
+            for (int k = tid; k < cw; k += NT) {
+                const double2 g = ((const double2*)l_group)[k / a.cpg], c = channel(a.weight ? a.weight[c0 + k] : 1.f, a.bias ? a.bias[c0 + k] : 0.f, g);
+                l_channel[k] = float2{(float)(n_all * c.x), (float)(c.y + 128.0 - (g.x + 128.0 * n_all) * c.x - 128.0 * rs)};
+            }
+            __syncthreads();
+            float f[VEC], h[VEC], most = 0.f;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                const int c = c0 + col * VEC + e;
-                const double2 g = l_group_d[(col * VEC + e) / a.cpg];
-                const double m = (a.weight ? (double)a.weight[c] : 1.0) * a.out_scale * g.y, o = (a.bias ? (double)a.bias[c] : 0.0) * a.out_scale + 0.5;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int p = base + row + i * rows;
-                    if (p >= p1) continue;
-                    double t = fma(n_all * P::i(data[i], e) - g.x, m, o);
-                    if (res) t += res[p * a.r_pixel + e] * a.res_scale;
-                    q[i][e] = (int)fmin(fmax(floor(t), (double)a.lo), (double)a.hi);
-                }
+                const float2 c = l_channel[min(col * VEC, cw - VEC) + e];
+                f[e] = c.x;
+                h[e] = c.y;
+                most = fmaxf(most, 256.f * fabsf(f[e]) + fabsf(h[e]));
+                if (!(fabsf(f[e]) < 1e30f) || !(fabsf(h[e]) < 1e30f)) most = 1e30f;
             }
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int p = base + row + i * rows;
-                if (p >= p1) continue;
-                if constexpr (VEC == 1) y[p * a.y_pixel] = (int8_t)q[i][0];
-                else {
+            // how far t can be off, in half steps of 2^-24: a byte times its rounded factor, the rounded offset, the sum, the sum with the residual (results past the bounds do not matter).
+            // t is kept half a unit inside the bounds: all that is cut off there has the bound as its result, and is not near a whole number
+            const float safe = 0.5f - 5.97e-8f * (most + 256.f * rs + 520.f);
+            const float lo = (float)(a.lo + 128) + 0.5f, hi = (float)(a.hi + 128) + 0.5f;
+            auto run = [&](auto res_tag) {
+                constexpr bool RES = decltype(res_tag)::value;
+                tiles(res_tag, [&](const raw& d, const raw& r) {
                     v4i o;
 #pragma unroll
-                    for (int e = 0; e < VEC; e += 4) o[e >> 2] = (int)pack4_i8(q[i][e], q[i][e + 1], q[i][e + 2], q[i][e + 3]);
-                    *(v4i*)(y + p * a.y_pixel) = o;
-                }
-            }
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t xd = (uint32_t)d[w] ^ 0x80808080u, xr = RES ? (uint32_t)r[w] ^ 0x80808080u : 0u;
+                        uint32_t q = 0;
+                        float far = 0.f;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int e = 4 * w + k;
+                            float t = fmaf((float)(xd >> (8 * k) & 255u), f[e], h[e]);
+                            if constexpr (RES) t = fmaf((float)(xr >> (8 * k) & 255u), rs, t);
+                            t = clamp_f32(t, lo, hi);
+                            const float part = __builtin_amdgcn_fractf(t);
+                            far = fmaxf(far, fabsf(part - 0.5f));
+                            q = __builtin_amdgcn_cvt_pk_u8_f32(t - part, k, q);
+                        }
+                        q ^= 0x80808080u;
+                        if (!(far < safe)) {                         // near a whole number
+                            q = 0;
+#pragma unroll 1
+                            for (int k = 0; k < 4; ++k) {
+                                const int e = 4 * w + k, c = c0 + col * VEC + e, v = (int)(signed char)((uint32_t)d[w] >> (8 * k)), rv = RES ? (int)(signed char)((uint32_t)r[w] >> (8 * k)) : 0;
+                                const double2 g = group_of(e);
+                                q |= ((uint32_t)in_64(v, rv, g.x, channel(a.weight ? a.weight[c] : 1.f, a.bias ? a.bias[c] : 0.f, g)) & 255u) << (8 * k);
+                            }
+                        }
+                        o[w] = (int)q;
+                    }
+                    return o;
+                });
+            };
+            if (has_res) run(std::true_type{});
+            else run(std::false_type{});
         }
     }
 }
 
+enum { NORM_LDS = 160 * 1024 };
 int gcd_i(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return a; }
 int log2_up(int v) { int k = 0; while ((1 << k) < v) ++k; return k; }
 
-// how a call is cut up: the kernel's window, its threads and vectors per lane, chunks of pixels (1: one launch)
-struct NormPlan { int vec, gpv, nt, nv, wv, wlog, windows, chunks, chunk_pixels; bool ok; };
+// how a call is cut up: the kernel's window, its threads and vectors per lane, chunks of pixels; split: two launches
+struct NormPlan { int vec, gpv, nt, nv, wv, wlog, windows, chunks, chunk_pixels; bool ok, split; };
 
-size_t norm_lds(int es, int gpv, int nt, int wlog, int window_groups)
+size_t norm_lds(int es, int gpv, int nt, int wlog, int window_groups, int window_channels)
 {
     const size_t cells = (size_t)(nt / std::max(64, 1 << wlog)) << wlog;
-    return (es == 2 ? 4 : 0) * cells + (es == 2 ? 8 : 16) * cells * gpv + 16 * (size_t)window_groups;
+    return (es == 2 ? 4 : 0) * cells + (es == 2 ? 8 : 16) * cells * gpv + 16 * (size_t)window_groups + (es == 1 ? 8 * (size_t)window_channels : 0);
 }
 
 bool plan_norm_vec(const NormArgs& a, int vec, NormPlan& p)
@@ -386,26 +506,41 @@ bool plan_norm_vec(const NormArgs& a, int vec, NormPlan& p)
         p.wlog = log2_up(p.wv);
         p.windows = (all + p.wv - 1) / p.wv;
     };
-    auto fits = [&] { return (1 << p.wlog) <= p.nt && norm_lds(es, p.gpv, p.nt, p.wlog, p.wv * vec / cpg) <= 65536; };
-    window(vec == 1 ? 64 : 8);
-    static const int forms[][2] = {{256, 1}, {256, 4}, {256, 16}, {1024, 8}, {1024, 16}};
-    for (const auto& f : forms) {
-        p.nt = f[0]; p.nv = f[1];
-        if (!fits() || (int64_t)p.nv * (p.nt >> p.wlog) < a.pixels) continue;
-        p.chunks = 1; p.chunk_pixels = a.pixels;
-        return true;
+    auto fits = [&] { return (1 << p.wlog) <= p.nt && norm_lds(es, p.gpv, p.nt, p.wlog, p.wv * vec / cpg, p.wv * vec) <= NORM_LDS; };
+    static const int forms[][2] = {{256, 1}, {256, 4}, {1024, 4}};
+    static const char* env = getenv("NORM");
+    const int mode = env ? atoi(env) : 0;
+    // one launch: 128 bytes of a pixel to a workgroup, or less where that makes too few workgroups or too much for one
+    bool found = false;
+    for (int want = vec == 1 ? 64 : 8; want >= (vec == 1 ? 16 : 2) && mode != 1; want /= 2) {
+        NormPlan t = p;
+        window(want);
+        for (const auto& f : forms) {
+            p.nt = f[0]; p.nv = f[1];
+            if (!fits() || (int64_t)p.nv * (p.nt >> p.wlog) < a.pixels) continue;
+            p.chunks = 1; p.chunk_pixels = a.pixels;
+            if (found && p.wlog == t.wlog) break;
+            found = true;
+            t = p;
+            break;
+        }
+        p = t;
+        if (found && (int64_t)a.b * p.windows >= 1024) break;
     }
+    if (found) return true;
     for (int want = 64; want >= 8; want /= 2) {
         window(want);
         p.nt = p.wlog > 8 ? 1024 : 256;
-        p.nv = 8;
+        p.nv = 8;                                                     // in two sets
         if (!fits()) continue;
         const int tile = p.nv * (p.nt >> p.wlog);                     // pixels a workgroup holds at once
-        const int64_t tiles = ((int64_t)a.pixels + tile - 1) / tile;
-        p.chunks = (int)std::min<int64_t>(tiles, 64);
+        const int64_t tiles = ((int64_t)a.pixels + tile - 1) / tile, units = (int64_t)a.b * p.windows;
+        static const char* u = getenv("UNITS");
+        p.chunks = (int)std::min<int64_t>(tiles, std::min<int64_t>(64, std::max<int64_t>(1, (u ? atoi(u) : 2048) / units)));
         const int64_t per = (tiles + p.chunks - 1) / p.chunks;
         p.chunk_pixels = (int)std::min<int64_t>(per * tile, a.pixels);
         p.chunks = (int)(((int64_t)a.pixels + p.chunk_pixels - 1) / p.chunk_pixels);
+        p.split = true;
         return true;
     }
     return false;
@@ -419,27 +554,28 @@ NormPlan plan_norm(const NormArgs& a, bool aligned)
     return p;
 }
 
-template <int ES, int VEC, int GPV, int NT, int NV, int MODE>
-hipError_t launch_norm_form(const NormKernelArgs& k, int b, hipStream_t s)
+template <int ES, int VEC, int GPV, int NT, int NV, int FORM>
+hipError_t launch_norm_form(const NormKernelArgs& k, hipStream_t s)
 {
-    const size_t lds = norm_lds(ES, GPV, NT, k.wlog, k.cw / k.cpg);
-    EE_LAUNCH((group_norm_kernel<ES, VEC, GPV, NT, NV, MODE>), dim3((unsigned)((int64_t)b * k.chunks * k.windows)), dim3(NT), (unsigned)lds, s, k);
+    static const hipError_t granted = hipFuncSetAttribute(reinterpret_cast<const void*>(&group_norm_kernel<ES, VEC, GPV, NT, NV, FORM>), hipFuncAttributeMaxDynamicSharedMemorySize, NORM_LDS);
+    if (granted != hipSuccess) return granted;
+    EE_LAUNCH((group_norm_kernel<ES, VEC, GPV, NT, NV, FORM>), dim3(xcd_grid(k.units)), dim3(NT), (unsigned)norm_lds(ES, GPV, NT, k.wlog, k.cw / k.cpg, k.cw), s, k);
     return hipGetLastError();
 }
 
 template <int ES, int VEC, int GPV>
-hipError_t launch_norm_gpv(const NormKernelArgs& k, const NormPlan& p, int b, hipStream_t s)
+hipError_t launch_norm_gpv(const NormKernelArgs& k, const NormPlan& p, hipStream_t s)
 {
-    if (p.chunks > 1) {
+    if (p.split) {
         if (p.nt == 256) {
-            const hipError_t e = launch_norm_form<ES, VEC, GPV, 256, 8, 1>(k, b, s);
-            return e == hipSuccess ? launch_norm_form<ES, VEC, GPV, 256, 8, 2>(k, b, s) : e;
+            const hipError_t e = launch_norm_form<ES, VEC, GPV, 256, 4, 1>(k, s);
+            return e == hipSuccess ? launch_norm_form<ES, VEC, GPV, 256, 4, 2>(k, s) : e;
         }
-        const hipError_t e = launch_norm_form<ES, VEC, GPV, 1024, 8, 1>(k, b, s);
-        return e == hipSuccess ? launch_norm_form<ES, VEC, GPV, 1024, 8, 2>(k, b, s) : e;
+        const hipError_t e = launch_norm_form<ES, VEC, GPV, 1024, 4, 1>(k, s);
+        return e == hipSuccess ? launch_norm_form<ES, VEC, GPV, 1024, 4, 2>(k, s) : e;
     }
-    if (p.nt == 256) return p.nv == 1 ? launch_norm_form<ES, VEC, GPV, 256, 1, 0>(k, b, s) : p.nv == 4 ? launch_norm_form<ES, VEC, GPV, 256, 4, 0>(k, b, s) : launch_norm_form<ES, VEC, GPV, 256, 16, 0>(k, b, s);
-    return p.nv == 8 ? launch_norm_form<ES, VEC, GPV, 1024, 8, 0>(k, b, s) : launch_norm_form<ES, VEC, GPV, 1024, 16, 0>(k, b, s);
+    if (p.nt == 256) return p.nv == 1 ? launch_norm_form<ES, VEC, GPV, 256, 1, 0>(k, s) : launch_norm_form<ES, VEC, GPV, 256, 4, 0>(k, s);
+    return launch_norm_form<ES, VEC, GPV, 1024, 4, 0>(k, s);
 }
 
 bool norm_aligned(const NormArgs& a)
@@ -456,7 +592,7 @@ bool group_norm_supported(const NormArgs& a) { return plan_norm(a, norm_aligned(
 bool group_norm_grid_fits(const NormArgs& a)
 {
     const NormPlan p = plan_norm(a, norm_aligned(a));
-    return (int64_t)a.b * p.chunks * p.windows < 1ll << 31;
+    return (int64_t)a.b * p.chunks * p.windows < 1ll << 28;
 }
 
 // a call whose alignment is not known yet may be cut either way
@@ -465,7 +601,7 @@ size_t group_norm_workspace(const NormArgs& a)
     size_t most = 0;
     for (const bool aligned : {false, true}) {
         const NormPlan p = plan_norm(a, aligned);
-        if (p.ok && p.chunks > 1) most = std::max(most, (size_t)a.b * p.chunks * a.groups * 16);
+        if (p.ok && p.split) most = std::max(most, (size_t)a.b * p.chunks * a.groups * 16);
     }
     return most;
 }
@@ -477,17 +613,17 @@ hipError_t launch_group_norm(const NormArgs& a, void* workspace, hipStream_t s)
     k.x = a.x; k.res = a.res; k.y = a.y; k.weight = a.weight; k.bias = a.bias; k.part = workspace;
     k.x_sample = a.x_sample; k.x_pixel = a.x_pixel; k.r_sample = a.res_sample; k.r_pixel = a.res_pixel; k.y_sample = a.y_sample; k.y_pixel = a.y_pixel;
     k.pixels = a.pixels; k.c = a.c; k.groups = a.groups; k.cpg = a.c / a.groups;
-    k.cw = p.wv * p.vec; k.wlog = p.wlog; k.windows = p.windows; k.chunks = p.chunks; k.chunk_pixels = p.chunk_pixels;
+    k.cw = p.wv * p.vec; k.wlog = p.wlog; k.windows = p.windows; k.chunks = p.chunks; k.chunk_pixels = p.chunk_pixels; k.units = a.b * p.chunks * p.windows;
     k.eps = a.eps; k.act = a.act;
     k.out_scale = std::ldexp(1.0, a.frac_bits); k.res_scale = std::ldexp(1.0, a.res_shift);
     k.lo = a.act == EE_ACT_NONE ? -128 : 0;
     k.hi = a.act == EE_ACT_RELU6 ? (int)std::min(127.0, 6.0 * k.out_scale) : 127;
     if (a.dtype == EE_I8) {
-        if (p.vec == 1) return launch_norm_gpv<1, 1, 1>(k, p, a.b, s);
-        return p.gpv == 1 ? launch_norm_gpv<1, 16, 1>(k, p, a.b, s) : p.gpv == 4 ? launch_norm_gpv<1, 16, 4>(k, p, a.b, s) : launch_norm_gpv<1, 16, 16>(k, p, a.b, s);
+        if (p.vec == 1) return launch_norm_gpv<1, 1, 1>(k, p, s);
+        return p.gpv == 1 ? launch_norm_gpv<1, 16, 1>(k, p, s) : p.gpv == 4 ? launch_norm_gpv<1, 16, 4>(k, p, s) : launch_norm_gpv<1, 16, 16>(k, p, s);
     }
-    if (p.vec == 1) return launch_norm_gpv<2, 1, 1>(k, p, a.b, s);
-    return p.gpv == 1 ? launch_norm_gpv<2, 8, 1>(k, p, a.b, s) : p.gpv == 4 ? launch_norm_gpv<2, 8, 4>(k, p, a.b, s) : launch_norm_gpv<2, 8, 8>(k, p, a.b, s);
+    if (p.vec == 1) return launch_norm_gpv<2, 1, 1>(k, p, s);
+    return p.gpv == 1 ? launch_norm_gpv<2, 8, 1>(k, p, s) : p.gpv == 4 ? launch_norm_gpv<2, 8, 4>(k, p, s) : launch_norm_gpv<2, 8, 8>(k, p, s);
 }
 
 }  // namespace ee
