@@ -82,16 +82,20 @@ struct View {
         r = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, pixels ? (pixels - 1) * pitch + channels * ES : 0, 0x00020000);
         off = live ? (unsigned)(row * pitch + col * VEC * ES) : 0x80000000u;
     }
-    __device__ __forceinline__ raw load(int step) const
+    // past: past the caches (non-temporal)
+    __device__ __forceinline__ raw load(int step, bool past = false) const
     {
-        if constexpr (VEC > 1) return __builtin_bit_cast(raw, __builtin_amdgcn_raw_buffer_load_b128(r, off + (unsigned)(step * pitch), 0, 0));
+        if constexpr (VEC > 1) return past ? __builtin_bit_cast(raw, __builtin_amdgcn_raw_buffer_load_b128(r, off + (unsigned)(step * pitch), 0, 2)) : __builtin_bit_cast(raw, __builtin_amdgcn_raw_buffer_load_b128(r, off + (unsigned)(step * pitch), 0, 0));
         else if constexpr (ES == 2) return __builtin_bit_cast(raw, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, off + (unsigned)(step * pitch), 0, 0));
         else return __builtin_bit_cast(raw, (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, off + (unsigned)(step * pitch), 0, 0));
     }
-    __device__ __forceinline__ void store(raw v, int step) const
+    __device__ __forceinline__ void store(raw v, int step, bool past = false) const
     {
         typedef unsigned v4u __attribute__((ext_vector_type(4)));
-        if constexpr (VEC > 1) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, v), r, off + (unsigned)(step * pitch), 0, 0);
+        if constexpr (VEC > 1) {
+            if (past) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, v), r, off + (unsigned)(step * pitch), 0, 2);
+            else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, v), r, off + (unsigned)(step * pitch), 0, 0);
+        }
         else if constexpr (ES == 2) __builtin_amdgcn_raw_buffer_store_b16(v, r, off + (unsigned)(step * pitch), 0, 0);
         else __builtin_amdgcn_raw_buffer_store_b8((uint8_t)v, r, off + (unsigned)(step * pitch), 0, 0);
     }
@@ -122,8 +126,8 @@ __device__ __forceinline__ void merge_lanes(Sums& s, int off, int)
 }
 
 // FORM 0: the whole sample's window in one workgroup, 1: statistics of a chunk, 2: merge the chunks of the sample, write one chunk.
-// GPV: partial results per column (each of VEC / GPV channels of one group)
-template <int ES, int VEC, int GPV, int NT, int NV, int FORM>
+// GPV: partial results per column (each of VEC / GPV channels of one group); PAST: y is written, and the residual read, past the caches
+template <int ES, int VEC, int GPV, int NT, int NV, int FORM, bool PAST>
 __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
 {
     using P = Pack<ES, VEC>;
@@ -160,12 +164,13 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
     // every group of the window, 2^sl lanes each that take its `entries` in turn: s = sum of get(group, entry); then f(group, s) in one lane
     auto per_group = [&](int entries, auto&& get, auto&& f) {
         int sl = 0;
-        while (sl < 6 && (1 << sl) < entries) ++sl;
+        while (sl < 6 && (1 << sl) < entries && wgroups << (sl + 1) <= NT) ++sl;      // all groups at once, if they are no more than threads
         const int lanes = 1 << sl, sub = tid & (lanes - 1);
         for (int g0 = 0; g0 < wgroups; g0 += NT >> sl) {
             const int g = g0 + (tid >> sl);
             stat_t s{};
             if (g < wgroups)
+#pragma unroll 4
                 for (int e = sub; e < entries; e += lanes) get(g, e, s);
 #pragma unroll 1
             for (int off = 1; off < lanes; off <<= 1) merge_lanes(s, off, lane);
@@ -336,13 +341,13 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
         auto residuals = [&](raw (&to)[BV], int i0) {
             if constexpr (RES)
 #pragma unroll
-                for (int i = 0; i < BV; ++i) to[i] = res.load(i0 + i * rows);
+                for (int i = 0; i < BV; ++i) to[i] = res.load(i0 + i * rows, PAST);
         };
         auto four = [&](raw* d, raw (&rr)[BV], int i0) {
 #pragma unroll
             for (int i = 0; i < BV; ++i) {
                 forget(d[i]);
-                y.store(f(d[i], rr[i]), i0 + i * rows);
+                y.store(f(d[i], rr[i]), i0 + i * rows, PAST);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
@@ -486,7 +491,7 @@ int gcd_i(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } retur
 int log2_up(int v) { int k = 0; while ((1 << k) < v) ++k; return k; }
 
 // how a call is cut up: the kernel's window, its threads and vectors per lane, chunks of pixels; split: two launches
-struct NormPlan { int vec, gpv, nt, nv, wv, wlog, windows, chunks, chunk_pixels; bool ok, split; };
+struct NormPlan { int vec, gpv, nt, nv, wv, wlog, windows, chunks, chunk_pixels, batch; bool ok, split, past; };
 
 size_t norm_lds(int es, int gpv, int nt, int wlog, int window_groups, int window_channels)
 {
@@ -508,11 +513,9 @@ bool plan_norm_vec(const NormArgs& a, int vec, NormPlan& p)
     };
     auto fits = [&] { return (1 << p.wlog) <= p.nt && norm_lds(es, p.gpv, p.nt, p.wlog, p.wv * vec / cpg, p.wv * vec) <= NORM_LDS; };
     static const int forms[][2] = {{256, 1}, {256, 4}, {1024, 4}};
-    static const char* env = getenv("NORM");
-    const int mode = env ? atoi(env) : 0;
-    // one launch: 128 bytes of a pixel to a workgroup, or less where that makes too few workgroups or too much for one
+    // one launch: 128 bytes of a pixel to a workgroup, or less (down to 32) where that makes too few workgroups or is more than one holds.  int8 64 x 14x14x1024, 64 bytes for 128: 22 -> 15 us
     bool found = false;
-    for (int want = vec == 1 ? 64 : 8; want >= (vec == 1 ? 16 : 2) && mode != 1; want /= 2) {
+    for (int want = vec == 1 ? 64 : 8; want >= (vec == 1 ? 16 : 2); want /= 2) {
         NormPlan t = p;
         window(want);
         for (const auto& f : forms) {
@@ -528,6 +531,8 @@ bool plan_norm_vec(const NormArgs& a, int vec, NormPlan& p)
         if (found && (int64_t)a.b * p.windows >= 1024) break;
     }
     if (found) return true;
+    // two launches, of whole pixels where they are up to 1 KiB.  Few long workgroups: what one does before its first result is worth tens of KB.  256 / 512 / 1024 / 2048 of them, bf16, us:
+    // 64 x 56x56x256 with residual 69, 68, 75, 79, 16 of these 24, 27, 31, 31; 256 x 112x112x64 225, 222, 224, 221
     for (int want = 64; want >= 8; want /= 2) {
         window(want);
         p.nt = p.wlog > 8 ? 1024 : 256;
@@ -535,8 +540,7 @@ bool plan_norm_vec(const NormArgs& a, int vec, NormPlan& p)
         if (!fits()) continue;
         const int tile = p.nv * (p.nt >> p.wlog);                     // pixels a workgroup holds at once
         const int64_t tiles = ((int64_t)a.pixels + tile - 1) / tile, units = (int64_t)a.b * p.windows;
-        static const char* u = getenv("UNITS");
-        p.chunks = (int)std::min<int64_t>(tiles, std::min<int64_t>(64, std::max<int64_t>(1, (u ? atoi(u) : 2048) / units)));
+        p.chunks = (int)std::min<int64_t>(tiles, std::min<int64_t>(64, std::max<int64_t>(1, 512 / units)));
         const int64_t per = (tiles + p.chunks - 1) / p.chunks;
         p.chunk_pixels = (int)std::min<int64_t>(per * tile, a.pixels);
         p.chunks = (int)(((int64_t)a.pixels + p.chunk_pixels - 1) / p.chunk_pixels);
@@ -546,31 +550,46 @@ bool plan_norm_vec(const NormArgs& a, int vec, NormPlan& p)
     return false;
 }
 
+// Two launches read x twice: so many samples at a time that the last-level cache (256 MB) still holds them for the second.  256 x 112x112x64 bf16 (411 MB) 233 us in one part, 213 in two, 243 in
+// four; 256 x 56x56x256 with residual 307, 276, 321
+int norm_batch(const NormArgs& a)
+{
+    const double bytes = (double)a.b * a.pixels * a.c * (a.dtype == EE_I8 ? 1 : 2);
+    const int parts = (int)std::min((double)a.b, std::ceil(bytes / (224.0 * 1048576.0)));
+    return parts > 1 ? (a.b + parts - 1) / parts : a.b;
+}
+
 NormPlan plan_norm(const NormArgs& a, bool aligned)
 {
+    NormArgs part = a;
+    part.b = norm_batch(a);
     NormPlan p{};
     const int full = a.dtype == EE_I8 ? 16 : 8;
-    p.ok = (aligned && a.c % full == 0 && plan_norm_vec(a, full, p)) || plan_norm_vec(a, 1, p);
+    p.ok = (aligned && a.c % full == 0 && plan_norm_vec(part, full, p)) || plan_norm_vec(part, 1, p);
+    p.batch = p.split ? part.b : a.b;
+    // a large result is written past the caches: left in them, writing it back would fall on the next kernel.  64 x 56x56x256 bf16 with residual, both launches 89 -> 77 us, 256 x 112x112x64 247 -> 232
+    p.past = (double)a.b * a.pixels * a.c * (a.dtype == EE_I8 ? 1 : 2) >= 64e6;
     return p;
 }
 
-template <int ES, int VEC, int GPV, int NT, int NV, int FORM>
+template <int ES, int VEC, int GPV, int NT, int NV, int FORM, bool PAST = false>
 hipError_t launch_norm_form(const NormKernelArgs& k, hipStream_t s)
 {
-    static const hipError_t granted = hipFuncSetAttribute(reinterpret_cast<const void*>(&group_norm_kernel<ES, VEC, GPV, NT, NV, FORM>), hipFuncAttributeMaxDynamicSharedMemorySize, NORM_LDS);
+    static const hipError_t granted = hipFuncSetAttribute(reinterpret_cast<const void*>(&group_norm_kernel<ES, VEC, GPV, NT, NV, FORM, PAST>), hipFuncAttributeMaxDynamicSharedMemorySize, NORM_LDS);
     if (granted != hipSuccess) return granted;
-    EE_LAUNCH((group_norm_kernel<ES, VEC, GPV, NT, NV, FORM>), dim3(xcd_grid(k.units)), dim3(NT), (unsigned)norm_lds(ES, GPV, NT, k.wlog, k.cw / k.cpg, k.cw), s, k);
+    EE_LAUNCH((group_norm_kernel<ES, VEC, GPV, NT, NV, FORM, PAST>), dim3(xcd_grid(k.units)), dim3(NT), (unsigned)norm_lds(ES, GPV, NT, k.wlog, k.cw / k.cpg, k.cw), s, k);
     return hipGetLastError();
 }
 
 template <int ES, int VEC, int GPV>
 hipError_t launch_norm_gpv(const NormKernelArgs& k, const NormPlan& p, hipStream_t s)
 {
+    if (p.split && p.nt == 256) {
+        const hipError_t e = launch_norm_form<ES, VEC, GPV, 256, 4, 1>(k, s);
+        if (e != hipSuccess) return e;
+        return p.past ? launch_norm_form<ES, VEC, GPV, 256, 4, 2, true>(k, s) : launch_norm_form<ES, VEC, GPV, 256, 4, 2>(k, s);
+    }
     if (p.split) {
-        if (p.nt == 256) {
-            const hipError_t e = launch_norm_form<ES, VEC, GPV, 256, 4, 1>(k, s);
-            return e == hipSuccess ? launch_norm_form<ES, VEC, GPV, 256, 4, 2>(k, s) : e;
-        }
         const hipError_t e = launch_norm_form<ES, VEC, GPV, 1024, 4, 1>(k, s);
         return e == hipSuccess ? launch_norm_form<ES, VEC, GPV, 1024, 4, 2>(k, s) : e;
     }
@@ -592,7 +611,7 @@ bool group_norm_supported(const NormArgs& a) { return plan_norm(a, norm_aligned(
 bool group_norm_grid_fits(const NormArgs& a)
 {
     const NormPlan p = plan_norm(a, norm_aligned(a));
-    return (int64_t)a.b * p.chunks * p.windows < 1ll << 28;
+    return (int64_t)p.batch * p.chunks * p.windows < 1ll << 28;
 }
 
 // a call whose alignment is not known yet may be cut either way
@@ -601,7 +620,7 @@ size_t group_norm_workspace(const NormArgs& a)
     size_t most = 0;
     for (const bool aligned : {false, true}) {
         const NormPlan p = plan_norm(a, aligned);
-        if (p.ok && p.split) most = std::max(most, (size_t)a.b * p.chunks * a.groups * 16);
+        if (p.ok && p.split) most = std::max(most, (size_t)p.batch * p.chunks * a.groups * 16);
     }
     return most;
 }
@@ -610,20 +629,24 @@ hipError_t launch_group_norm(const NormArgs& a, void* workspace, hipStream_t s)
 {
     const NormPlan p = plan_norm(a, norm_aligned(a));
     NormKernelArgs k{};
-    k.x = a.x; k.res = a.res; k.y = a.y; k.weight = a.weight; k.bias = a.bias; k.part = workspace;
+    k.weight = a.weight; k.bias = a.bias; k.part = workspace;
     k.x_sample = a.x_sample; k.x_pixel = a.x_pixel; k.r_sample = a.res_sample; k.r_pixel = a.res_pixel; k.y_sample = a.y_sample; k.y_pixel = a.y_pixel;
     k.pixels = a.pixels; k.c = a.c; k.groups = a.groups; k.cpg = a.c / a.groups;
-    k.cw = p.wv * p.vec; k.wlog = p.wlog; k.windows = p.windows; k.chunks = p.chunks; k.chunk_pixels = p.chunk_pixels; k.units = a.b * p.chunks * p.windows;
+    k.cw = p.wv * p.vec; k.wlog = p.wlog; k.windows = p.windows; k.chunks = p.chunks; k.chunk_pixels = p.chunk_pixels;
     k.eps = a.eps; k.act = a.act;
     k.out_scale = std::ldexp(1.0, a.frac_bits); k.res_scale = std::ldexp(1.0, a.res_shift);
     k.lo = a.act == EE_ACT_NONE ? -128 : 0;
     k.hi = a.act == EE_ACT_RELU6 ? (int)std::min(127.0, 6.0 * k.out_scale) : 127;
-    if (a.dtype == EE_I8) {
-        if (p.vec == 1) return launch_norm_gpv<1, 1, 1>(k, p, s);
-        return p.gpv == 1 ? launch_norm_gpv<1, 16, 1>(k, p, s) : p.gpv == 4 ? launch_norm_gpv<1, 16, 4>(k, p, s) : launch_norm_gpv<1, 16, 16>(k, p, s);
+    const int64_t es = a.dtype == EE_I8 ? 1 : 2;
+    auto at = [&](const void* base, int b, int64_t sample) { return base ? (void*)((char*)base + b * sample * es) : nullptr; };
+    for (int b = 0; b < a.b; b += p.batch) {
+        k.x = at(a.x, b, a.x_sample); k.res = at(a.res, b, a.res_sample); k.y = at(a.y, b, a.y_sample);
+        k.units = std::min(p.batch, a.b - b) * p.chunks * p.windows;
+        const hipError_t e = a.dtype == EE_I8 ? (p.vec == 1 ? launch_norm_gpv<1, 1, 1>(k, p, s) : p.gpv == 1 ? launch_norm_gpv<1, 16, 1>(k, p, s) : p.gpv == 4 ? launch_norm_gpv<1, 16, 4>(k, p, s) : launch_norm_gpv<1, 16, 16>(k, p, s))
+                           : p.vec == 1 ? launch_norm_gpv<2, 1, 1>(k, p, s) : p.gpv == 1 ? launch_norm_gpv<2, 8, 1>(k, p, s) : p.gpv == 4 ? launch_norm_gpv<2, 8, 4>(k, p, s) : launch_norm_gpv<2, 8, 8>(k, p, s);
+        if (e != hipSuccess) return e;
     }
-    if (p.vec == 1) return launch_norm_gpv<2, 1, 1>(k, p, s);
-    return p.gpv == 1 ? launch_norm_gpv<2, 8, 1>(k, p, s) : p.gpv == 4 ? launch_norm_gpv<2, 8, 4>(k, p, s) : launch_norm_gpv<2, 8, 8>(k, p, s);
+    return hipSuccess;
 }
 
 }  // namespace ee
