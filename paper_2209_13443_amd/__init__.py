@@ -5,7 +5,9 @@ PyTorch supplies device memory (tensors) and the HIP stream; there is no CPU fal
 shared library is missing the import of this module fails.
 """
 import ctypes as C
+import functools
 import os
+from operator import index
 
 import numpy as np
 import torch  # noqa: F401  -- first: libee.so must bind to the HIP runtime PyTorch has already loaded
@@ -399,29 +401,45 @@ def _need(ok, what, code=EE_ERR_ARG):
         raise e
 
 
-def _on(device, f):
-    """f(stream handle) with `device` current."""
-    if device.index == torch.cuda.current_device():
-        return f(torch.cuda.current_stream().cuda_stream)
-    with torch.cuda.device(device):
-        return f(torch.cuda.current_stream().cuda_stream)
+# torch.cuda.current_stream() builds an object for this number: 2.6 us of a call of 8
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _tensor(t, name, dtypes, device):
-    _need(isinstance(t, torch.Tensor) and t.dtype in dtypes, f"{name} has to be a tensor of {' or '.join(str(d) for d in dtypes)}", EE_ERR_UNSUPPORTED)
-    _need(t.device == device and device.type == "cuda", f"{name} has to be on the GPU, all tensors on the same one")
+def _on(device, f, *args):
+    """f(*args, handle of the device's current stream) with `device` (its index) current."""
+    if device == torch.cuda.current_device():
+        _chk(f(*args, _stream_of(device)))
+    else:
+        with torch.cuda.device(device):
+            _chk(f(*args, _stream_of(device)))
 
 
-def _pixels(t, name):
+def _tensor(t, name, dtypes, device=None):
+    """t's device index (device: the one it has to be)."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+        _need(False, f"{name} has to be a tensor of {' or '.join(str(d) for d in dtypes)}", EE_ERR_UNSUPPORTED)
+    at = t.get_device() if t.is_cuda else -1
+    _need(at >= 0 and (device is None or at == device), "tensors have to be on the GPU, all on the same one")
+    return at
+
+
+def _pixels(shape, stride, name):
     """(samples, pixels, channels, sample stride, pixel stride) of [b, ..., c]; the dimensions between have to lie behind one another."""
-    _need(t.dim() >= 2 and (t.shape[-1] == 1 or t.stride(-1) == 1), f"{name} has to be [samples, ..., channels] with neighbouring channels")
+    _need(len(shape) >= 2 and (shape[-1] == 1 or stride[-1] == 1), f"{name} has to be [samples, ..., channels] with neighbouring channels")
     pixels, step = 1, 0
-    for n, s in zip(t.shape[-2:0:-1], t.stride()[-2:0:-1]):
+    for n, s in zip(shape[-2:0:-1], stride[-2:0:-1]):
         if n > 1:
             _need(step == 0 or s == step * pixels, f"the pixels of {name} have to lie one stride apart")
             step = step or s
         pixels *= n
-    return t.shape[0], pixels, t.shape[-1], t.stride(0), step or t.shape[-1]
+    return shape[0], pixels, shape[-1], stride[0], step or shape[-1]
+
+
+def _rows(shape, stride, name):
+    """(samples, rows of a sample, channels, stride of the rows) where all rows lie one stride apart."""
+    b, inner, c, sample, pixel = _pixels(shape, stride, name)
+    _need(inner == 1 or b <= 1 or sample == inner * pixel, f"the rows of {name} have to lie one stride apart")
+    return b, inner, c, c if b * inner <= 1 else sample if inner == 1 else pixel
 
 
 def _workspace(bytes_, device):
@@ -432,38 +450,67 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _layout(t):
+    return None if t is None else (t.shape, t.stride())
+
+
+# What follows from shapes and strides alone is worked out once for each of them: 3 to 5 us of a call.
+
+@functools.lru_cache(maxsize=1024)
+def _norm_plan(dtype, x, out, residual, weight, bias, groups, eps, act, frac_bits, res_shift):
+    b, pixels, c, sample, pixel = _pixels(*x, "x")
+    y = (b, pixels, c, pixels * c, c)
+    if out is not None:
+        y = _pixels(*out, "out")
+        _need(out[0] == x[0], "out has to have the shape of x")
+    r = (0, 0, 0, 0, 0)
+    if residual is not None:
+        _need(residual[0] == x[0], "residual has to have the shape of x")
+        r = _pixels(*residual, "residual")
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        _need(t is None or t[0] == (c,) and (c == 1 or t[1] == (1,)), f"{name} has to be dense [channels]")
+    _need(act in ACTS, f"act has to be one of {', '.join(ACTS)}")
+    d = NormDesc(EE_I8 if dtype == torch.int8 else EE_BF16, ACTS[act], b, pixels, c, groups, frac_bits, res_shift, eps, 0, sample, pixel, r[3], r[4], y[3], y[4])
+    need = C.c_int64()
+    _chk(_lib.ee_group_norm_workspace(C.byref(d), C.byref(need)))
+    return C.byref(d), need.value
+
+
 def group_norm(x, groups, weight=None, bias=None, eps=1e-5, act="none", residual=None, frac_bits=0, res_shift=0, out=None):
     """ee_group_norm: act(group norm of x + residual) on x[b, ..., c] (int8, bfloat16 or int16 holding bf16 bits; any sample stride, one pixel stride, channel slices included).
     weight, bias: float32 [c].  act: "none", "relu", "relu6", "silu" (not int8).  int8: the result is in units of 2^-frac_bits, the residual enters times 2^res_shift."""
-    dev = x.device
-    _tensor(x, "x", (torch.bfloat16, torch.int8, torch.int16), dev)
-    b, pixels, c, sample, pixel = _pixels(x, "x")
-    if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        y = (b, pixels, c, pixels * c, c)
-    else:
+    dev = _tensor(x, "x", (torch.bfloat16, torch.int8, torch.int16))
+    if out is not None:
         _tensor(out, "out", (x.dtype,), dev)
-        y = _pixels(out, "out")
-    _need(out.shape == x.shape, "out has to have the shape of x")
-    r = (0, 0, 0, 0, 0)
     if residual is not None:
         _tensor(residual, "residual", (x.dtype,), dev)
-        _need(residual.shape == x.shape, "residual has to have the shape of x")
-        r = _pixels(residual, "residual")
-    for t, name in ((weight, "weight"), (bias, "bias")):
-        if t is not None:
-            _tensor(t, name, (torch.float32,), dev)
-            _need(t.shape == (c,) and t.is_contiguous(), f"{name} has to be dense [channels]")
-    _need(act in ACTS, f"act has to be one of {', '.join(ACTS)}")
-    d = NormDesc(EE_I8 if x.dtype == torch.int8 else EE_BF16, ACTS[act], b, pixels, c, groups, frac_bits, res_shift, eps, 0, sample, pixel, r[3], r[4], y[3], y[4])
-    need = C.c_int64()
-    _chk(_lib.ee_group_norm_workspace(C.byref(d), C.byref(need)))
-
-    def call(stream):
-        ws = _workspace(need.value, dev)
-        _chk(_lib.ee_group_norm(C.byref(d), x.data_ptr(), _ptr(weight), _ptr(bias), _ptr(residual), out.data_ptr(), _ptr(ws), need.value, stream))
-    _on(dev, call)
+    if weight is not None:
+        _tensor(weight, "weight", (torch.float32,), dev)
+    if bias is not None:
+        _tensor(bias, "bias", (torch.float32,), dev)
+    desc, need = _norm_plan(x.dtype, _layout(x), _layout(out), _layout(residual), _layout(weight), _layout(bias), index(groups), float(eps), act, index(frac_bits), index(res_shift))
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    ws = _workspace(need, x.device)
+    _on(dev, _lib.ee_group_norm, desc, x.data_ptr(), _ptr(weight), _ptr(bias), _ptr(residual), out.data_ptr(), _ptr(ws), need)
     return out
+
+
+@functools.lru_cache(maxsize=1024)
+def _adapter_plan(ci, co, adapters, rank, x, ids, offsets, out):
+    if offsets is not None:
+        _need(len(x[0]) == 2 and len(offsets[0]) == 1 and offsets[0][0] >= 1 and (offsets[0][0] == 1 or offsets[1] == (1,)), "offsets go with x [rows, ci]")
+    b, inner, channels, ldx = _rows(*x, "x")
+    _need(channels == ci, "x has to have ci channels")
+    slots, per = (b, inner) if offsets is None else (offsets[0][0] - 1, 0)
+    _need(ids is None or ids[0] == (slots,) and (slots <= 1 or ids[1] == (1,)), "ids has to be dense [slots]")
+    ldy = co
+    if out is not None:
+        _need(out[0] == x[0][:-1] + (co,), "out has to have the shape of x with co channels")
+        ldy = _rows(*out, "out")[3]
+    dims, need = AdapterDims(ci, co, adapters, rank), C.c_int64()
+    _chk(_lib.ee_adapter_workspace(C.byref(dims), b * inner, C.byref(need)))
+    return b * inner, slots, per, ldx, ldy, need.value
 
 
 class AdapterProjection:
@@ -471,12 +518,12 @@ class AdapterProjection:
     Room for `adapters` adapters of rank <= `rank`; load() puts one in (also between calls), unload() takes it out."""
 
     def __init__(self, weight, bias=None, adapters=0, rank=16):
+        at = _tensor(weight, "weight", (torch.bfloat16,))
         dev = weight.device
-        _tensor(weight, "weight", (torch.bfloat16,), dev)
         _need(weight.dim() == 2 and weight.stride(1) == 1, "weight has to be [co, ci] with dense rows")
         co, ci = weight.shape
         if bias is not None:
-            _tensor(bias, "bias", (torch.float32,), dev)
+            _tensor(bias, "bias", (torch.float32,), at)
             _need(bias.shape == (co,) and bias.is_contiguous(), "bias has to be dense [co]")
         self.device, self.ci, self.co, self.adapters, self.rank = dev, ci, co, adapters, rank
         self._dims = AdapterDims(ci, co, adapters, rank)
@@ -484,94 +531,72 @@ class AdapterProjection:
         _chk(_lib.ee_adapter_bytes(C.byref(self._dims), C.byref(packed), C.byref(pool)))
         self._packed = torch.empty(packed.value, dtype=torch.uint8, device=dev)
         self._pool = torch.zeros(pool.value, dtype=torch.uint8, device=dev)
-        _on(dev, lambda s: _chk(_lib.ee_adapter_pack(C.byref(self._dims), weight.data_ptr(), weight.stride(0), _ptr(bias), self._packed.data_ptr(), s)))
+        _on(at, _lib.ee_adapter_pack, C.byref(self._dims), weight.data_ptr(), weight.stride(0), _ptr(bias), self._packed.data_ptr())
 
     def load(self, i, a, b, scale=1.0):
         """Adapter i becomes scale * b a (a: bfloat16 [r, ci], b: bfloat16 [co, r], r <= rank), for the calls behind this one on its stream."""
         for t, name in ((a, "a"), (b, "b")):
-            _tensor(t, name, (torch.bfloat16,), self.device)
+            _tensor(t, name, (torch.bfloat16,), self.device.index)
             _need(t.dim() == 2 and t.stride(1) == 1 or t.shape[1:] == (1,), f"{name} has to have dense rows")
         r = a.shape[0]
         _need(a.shape == (r, self.ci) and b.shape == (self.co, r), "a has to be [r, ci] and b [co, r]")
-        _on(self.device, lambda s: _chk(_lib.ee_adapter_load(C.byref(self._dims), i, r, a.data_ptr(), a.stride(0), b.data_ptr(), b.stride(0), scale, self._pool.data_ptr(), s)))
+        _on(self.device.index, _lib.ee_adapter_load, C.byref(self._dims), i, r, a.data_ptr(), a.stride(0), b.data_ptr(), b.stride(0), scale, self._pool.data_ptr())
 
     def unload(self, i):
-        _on(self.device, lambda s: _chk(_lib.ee_adapter_load(C.byref(self._dims), i, 0, None, 0, None, 0, 0.0, self._pool.data_ptr(), s)))
+        _on(self.device.index, _lib.ee_adapter_load, C.byref(self._dims), i, 0, None, 0, None, 0, 0.0, self._pool.data_ptr())
 
     def __call__(self, x, ids=None, offsets=None, out=None, dtype=torch.bfloat16):
         """x: bfloat16 [slots, ..., ci] or, with offsets (int32 [slots + 1]), [rows, ci] with the rows of slot s at offsets[s]..offsets[s + 1]; ids: int32 [slots], the adapter of
         every slot, outside [0, adapters): none.  Returns bfloat16 or float32 (dtype) with co in place of ci."""
-        dev = self.device
+        dev = self.device.index
         _tensor(x, "x", (torch.bfloat16,), dev)
         if offsets is not None:
             _tensor(offsets, "offsets", (torch.int32,), dev)
-            _need(x.dim() == 2 and offsets.dim() == 1 and offsets.numel() >= 1 and offsets.is_contiguous(), "offsets go with x [rows, ci]")
-            slots, per = offsets.numel() - 1, 0
-        b, inner, ci, sample, pixel = _pixels(x, "x")
-        if offsets is None:
-            slots, per = b, inner
-        if inner == 1:
-            pixel = sample
-        else:
-            _need(b <= 1 or sample == inner * pixel, "the rows of x have to lie one stride apart")
-        rows, ldx = b * inner, pixel if b * inner > 1 else ci
-        _need(ci == self.ci, "x has to have ci channels")
         if ids is not None:
             _tensor(ids, "ids", (torch.int32,), dev)
-            _need(ids.shape == (slots,) and ids.is_contiguous(), "ids has to be dense [slots]")
         _need(dtype in (torch.bfloat16, torch.float32), "results are bfloat16 or float32", EE_ERR_UNSUPPORTED)
-        shape = x.shape[:-1] + (self.co,)
-        if out is None:
-            out = torch.empty(shape, dtype=dtype, device=dev)
-            ldy = self.co
-        else:
+        if out is not None:
             _tensor(out, "out", (dtype,), dev)
-            _need(out.shape == shape, "out has to have the shape of x with co channels")
-            ob, oi, _, os_, op = _pixels(out, "out")
-            _need(oi == 1 or ob <= 1 or os_ == oi * op, "the rows of out have to lie one stride apart")
-            ldy = (os_ if oi == 1 else op) if ob * oi > 1 else self.co
-        need = C.c_int64()
-        _chk(_lib.ee_adapter_workspace(C.byref(self._dims), rows, C.byref(need)))
-
-        def call(stream):
-            ws = _workspace(need.value, dev)
-            c = AdapterCall(self._packed.data_ptr(), self._pool.data_ptr(), x.data_ptr(), out.data_ptr(), _ptr(ids), _ptr(offsets), ldx, ldy, rows, slots, per,
-                            int(dtype == torch.float32), _ptr(ws), need.value)
-            _chk(_lib.ee_adapter_project(C.byref(self._dims), C.byref(c), stream))
-        _on(dev, call)
+        rows, slots, per, ldx, ldy, need = _adapter_plan(self.ci, self.co, self.adapters, self.rank, _layout(x), _layout(ids), _layout(offsets), _layout(out))
+        if out is None:
+            out = torch.empty(x.shape[:-1] + (self.co,), dtype=dtype, device=self.device)
+        ws = _workspace(need, self.device)
+        c = AdapterCall(self._packed.data_ptr(), self._pool.data_ptr(), x.data_ptr(), out.data_ptr(), _ptr(ids), _ptr(offsets), ldx, ldy, rows, slots, per,
+                        dtype == torch.float32, _ptr(ws), need)
+        _on(dev, _lib.ee_adapter_project, C.byref(self._dims), C.byref(c))
         return out
+
+
+@functools.lru_cache(maxsize=1024)
+def _verify_plan(p, draft, u, q, lengths):
+    dense = lambda t: t[0][-1] <= 1 or t[1][-1] == 1
+    _need(len(draft[0]) == 2 and len(p[0]) == 3, "draft has to be [b, k], target_probs [b, k + 1, v]")
+    (b, k), v = draft[0], p[0][2]
+    _need(p[0][:2] == (b, k + 1) and u[0] == (b, k + 1), "target_probs and u have to have k + 1 rows a sequence")
+    _need(dense(p) and dense(draft) and dense(u), "the last dimension has to be dense")
+    _need(q is None or q[0] == (b, k, v) and dense(q), "draft_probs has to be [b, k, v] with dense rows")
+    _need(lengths is None or lengths[0] == (b,) and (b <= 1 or lengths[1] == (1,)), "lengths has to be dense [b]")
+    need = C.c_int64()
+    _chk(_lib.ee_verify_workspace(b, k, v, C.byref(need)))
+    return b, k, v, (draft[1][0], u[1][0], p[1][0], p[1][1]) + ((0, 0) if q is None else q[1][:2]), need.value
 
 
 def verify_draft(draft, target_probs, u, draft_probs=None, lengths=None):
     """ee_verify_draft: (accepted int32 [b], tokens int32 [b, k + 1]) for draft int32 [b, k] against target_probs [b, k + 1, v] (float32 or bfloat16), drawn from draft_probs
     [b, k, v] (same type; None: certain), with the random numbers u float32 [b, k + 1] in [0, 1).  lengths int32 [b]: drafts per sequence, < 0: an empty slot."""
-    dev = target_probs.device
-    _tensor(target_probs, "target_probs", (torch.float32, torch.bfloat16), dev)
-    _tensor(draft, "draft", (torch.int32,), dev)
-    _tensor(u, "u", (torch.float32,), dev)
-    _need(draft.dim() == 2 and target_probs.dim() == 3, "draft has to be [b, k], target_probs [b, k + 1, v]")
-    b, k = draft.shape
-    v = target_probs.shape[2]
-    _need(target_probs.shape[:2] == (b, k + 1) and u.shape == (b, k + 1), "target_probs and u have to have k + 1 rows a sequence")
-    dense = lambda t: t.shape[-1] <= 1 or t.stride(-1) == 1
-    _need(dense(target_probs) and dense(draft) and dense(u), "the last dimension has to be dense")
-    q_seq = q_row = 0
+    at = _tensor(target_probs, "target_probs", (torch.float32, torch.bfloat16))
+    _tensor(draft, "draft", (torch.int32,), at)
+    _tensor(u, "u", (torch.float32,), at)
     if draft_probs is not None:
-        _tensor(draft_probs, "draft_probs", (target_probs.dtype,), dev)
-        _need(draft_probs.shape == (b, k, v) and dense(draft_probs), "draft_probs has to be [b, k, v] with dense rows")
-        q_seq, q_row = draft_probs.stride(0), draft_probs.stride(1)
+        _tensor(draft_probs, "draft_probs", (target_probs.dtype,), at)
     if lengths is not None:
-        _tensor(lengths, "lengths", (torch.int32,), dev)
-        _need(lengths.shape == (b,) and lengths.is_contiguous(), "lengths has to be dense [b]")
+        _tensor(lengths, "lengths", (torch.int32,), at)
+    b, k, v, strides, need = _verify_plan(_layout(target_probs), _layout(draft), _layout(u), _layout(draft_probs), _layout(lengths))
+    dev = target_probs.device
     accepted = torch.empty(b, dtype=torch.int32, device=dev)
-    tokens = torch.empty(b, k + 1, dtype=torch.int32, device=dev)
-    need = C.c_int64()
-    _chk(_lib.ee_verify_workspace(b, k, v, C.byref(need)))
-
-    def call(stream):
-        ws = _workspace(need.value, dev)
-        c = VerifyCall(draft.data_ptr(), target_probs.data_ptr(), _ptr(draft_probs), u.data_ptr(), _ptr(lengths), accepted.data_ptr(), tokens.data_ptr(), draft.stride(0), u.stride(0),
-                       target_probs.stride(0), target_probs.stride(1), q_seq, q_row, b, k, v, int(target_probs.dtype == torch.float32), _ptr(ws), need.value)
-        _chk(_lib.ee_verify_draft(C.byref(c), stream))
-    _on(dev, call)
+    tokens = torch.empty((b, k + 1), dtype=torch.int32, device=dev)
+    ws = _workspace(need, dev)
+    c = VerifyCall(draft.data_ptr(), target_probs.data_ptr(), _ptr(draft_probs), u.data_ptr(), _ptr(lengths), accepted.data_ptr(), tokens.data_ptr(), *strides, b, k, v,
+                   target_probs.dtype == torch.float32, _ptr(ws), need)
+    _on(at, _lib.ee_verify_draft, C.byref(c))
     return accepted, tokens
