@@ -24,7 +24,7 @@ struct AdapterKernelArgs {
     const int* ids; const int* offsets; int* row_ids; uint16_t* u;
     const uint16_t* zeros;                                           // 16 readable zero bytes
     int64_t ldx, ldy;
-    int rows, slots, per, ci, co, kp, np, rp, ra, adapters, out_f32, parts;      // parts: bf16 numbers that make up an element of u; 0: it is a float
+    int rows, slots, per, ci, co, kp, np, rp, ra, adapters, out_f32, parts, splits;      // parts: bf16 numbers that make up an element of u; 0: it is `splits` floats, to be added
 };
 
 // ---- layouts -----------------------------------------------------------------------------------------------------------------
@@ -78,6 +78,7 @@ __device__ __forceinline__ int adapter_of(const AdapterKernelArgs& a, int row, c
     return (unsigned)id < (unsigned)a.adapters ? id : -1;
 }
 
+enum { SPLITS = 4 };                 // few rows: workgroups that may share an adapter's first half
 enum { OFFSETS_LDS = 2048 };         // up to so many offsets are searched in LDS, more where they lie
 
 // u of ROWS rows (16 or 32: a matrix instruction's), RT x ROWS rows of the adapters' first halves at a time.  Eight wavefronts share the columns of x, 64 at a time, and add up through LDS.
@@ -87,6 +88,7 @@ enum { OFFSETS_LDS = 2048 };         // up to so many offsets are searched in LD
 template <int ROWS, int RT>
 __global__ __launch_bounds__(512) void adapter_shrink_kernel(AdapterKernelArgs a, int blocks, int ords)
 {
+    const int split = blockIdx.z;
     constexpr int NW = 8, KB = 512 / ROWS, GU = 64 / KB, XL = ROWS == 32 ? 4 : GU;       // KB: columns of a matrix instruction, GU: of them in 64, XL: loads of x a lane makes for them
     typedef typename std::conditional<ROWS == 32, v16f, v4f>::type acc_t;
     constexpr int SUM = NW * ROWS * (ROWS + 1) * 4, TURN = ROWS == 32 ? NW * 4096 : 0;
@@ -104,7 +106,7 @@ __global__ __launch_bounds__(512) void adapter_shrink_kernel(AdapterKernelArgs a
     if (tid < ROWS) {
         const int m = r0 + tid, id = m < a.rows ? adapter_of(a, m, in_lds ? l_off : a.offsets) : -2;
         l_id[tid] = id;
-        if (m < a.rows && ord == 0 && blockIdx.y == 0) a.row_ids[m] = id;
+        if (m < a.rows && ord == 0 && blockIdx.y == 0 && split == 0) a.row_ids[m] = id;
     }
     __syncthreads();
     const int id = l_id[frow];
@@ -167,11 +169,12 @@ __global__ __launch_bounds__(512) void adapter_shrink_kernel(AdapterKernelArgs a
                     else acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, wv[B][t][u]), __builtin_bit_cast(v8bf, xo[u]), acc[t], 0, 0, 0);
                 }
         };
-        load(std::integral_constant<int, 0>{}, wave);
-        for (int c = wave; c < chunks; c += 2 * NW) {
-            load(std::integral_constant<int, 1>{}, c + NW);
+        const int next = NW * a.splits;
+        load(std::integral_constant<int, 0>{}, wave + NW * split);
+        for (int c = wave + NW * split; c < chunks; c += 2 * next) {
+            load(std::integral_constant<int, 1>{}, c + next);
             multiply(std::integral_constant<int, 0>{});
-            load(std::integral_constant<int, 0>{}, c + 2 * NW);
+            load(std::integral_constant<int, 0>{}, c + 2 * next);
             multiply(std::integral_constant<int, 1>{});                          // past the end: zeros
         }
 #pragma unroll
@@ -188,7 +191,7 @@ __global__ __launch_bounds__(512) void adapter_shrink_kernel(AdapterKernelArgs a
 #pragma unroll
                     for (int q = 0; q < NW; ++q) v += l_sum[q][row][r];
                     v *= scale;
-                    if (a.parts == 0) ((float*)a.u)[(int64_t)(r0 + row) * a.rp + rank0 + t * ROWS + r] = v;
+                    if (a.parts == 0) ((float*)a.u)[((int64_t)split * a.rows + r0 + row) * a.rp + rank0 + t * ROWS + r] = v;
                     else {
                         uint16_t* const u = a.u + (int64_t)(r0 + row) * a.parts * a.rp + rank0 + t * ROWS + r;
                         for (int p = 0; p < a.parts; ++p) {
@@ -247,21 +250,21 @@ __global__ __launch_bounds__(512) void adapter_rows_project_kernel(AdapterKernel
     constexpr int J = MT == 4 ? 2 : 1;
     const int o = nb * 16 + (tid & 15);
     int id[J];
-    const v4f* u[J];
+    const float* u[J];
     const uint16_t* b[J];
-    v4f uv[J][4];
+    float uv[J][SPLITS];
     v4i bv[J][2];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         const int row = (tid >> 4) + 32 * j, m = m0 + row;
         id[j] = row < 16 * MT && m < a.rows ? a.row_ids ? a.row_ids[m] : -1 : -2;
-        u[j] = (const v4f*)((const float*)a.u + (int64_t)m * a.rp);
+        u[j] = (const float*)a.u + (int64_t)m * a.rp + (tid & 15);
         b[j] = a.b + (((int64_t)id[j] * (a.np / 32) + (nb >> 1)) * (a.rp / 16) * 64 + (nb & 1) * 16 + (tid & 15)) * 8;
     }
     auto load_adapter = [&](int j, int r) {
         if (id[j] < 0) return;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) uv[j][e] = u[j][r / 4 + e];
+        for (int e = 0; e < SPLITS; ++e) uv[j][e] = e < a.splits ? u[j][e * (int64_t)a.rows * a.rp + r] : 0.f;
 #pragma unroll
         for (int e = 0; e < 2; ++e) bv[j][e] = *(const v4i*)(b[j] + (r / 16 * 64 + e * 32) * 8);
     };
@@ -283,20 +286,24 @@ __global__ __launch_bounds__(512) void adapter_rows_project_kernel(AdapterKernel
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         const int row = (tid >> 4) + 32 * j;
-        if (id[j] == -2 || o >= a.co) continue;
+        if (id[j] == -2) continue;
         float v = bias;
 #pragma unroll
         for (int q = 0; q < NW; ++q) v += l_sum[q][row][tid & 15];
         if (id[j] >= 0)
             for (int r = 0; r < a.rp; r += 16) {
                 if (r) load_adapter(j, r);
+                float sum = uv[j][0];                                            // of element r + tid % 16; the row's sixteen threads show them to each other
+#pragma unroll
+                for (int e = 1; e < SPLITS; ++e) sum += uv[j][e];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const uint32_t two = (uint32_t)bv[j][e >> 2][e & 3];
-                    v = fmaf(uv[j][e >> 1][2 * e & 3], __uint_as_float(two << 16), v);
-                    v = fmaf(uv[j][e >> 1][(2 * e & 3) + 1], __uint_as_float(two & 0xFFFF0000u), v);
+                    v = fmaf(__shfl(sum, 2 * e, 16), __uint_as_float(two << 16), v);
+                    v = fmaf(__shfl(sum, 2 * e + 1, 16), __uint_as_float(two & 0xFFFF0000u), v);
                 }
             }
+        if (o >= a.co) continue;
         const int m = m0 + row;
         if (a.out_f32) ((float*)a.y)[m * a.ldy + o] = v;
         else ((uint16_t*)a.y)[m * a.ldy + o] = __builtin_bit_cast(uint16_t, (__bf16)v);
@@ -549,6 +556,10 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
 }
 
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+int64_t u_bytes(int64_t rows) { return rows <= 1024 ? 4 * SPLITS : 6; }      // of an element of u
+// Few rows leave most CUs idle in the first half, where what a workgroup reads is a chain: up to four share the columns.  One / two / four, both launches, us: 4096 -> 4096 12 rows 15.7 / 13.5 / 12.5;
+// 2048 -> 1000 64 rows 11.5 / 10.4 / 10.0, 128 rows 13.5 / 12.5 / 13.4, 256 rows 18.5 / 18.9 / 20.5; 512 -> 1000 no difference
+int splits_of(const AdapterKernelArgs& k) { return k.parts || k.rows > 1024 ? 1 : std::clamp(std::min(k.kp / 512, 256 / k.rows), 1, (int)SPLITS); }
 
 struct AdapterSizes {       // in bytes; everything a multiple of 256
     int64_t kp, np, rp, ra, w, bias, a, b, scale;          // rp, ra: the rank as a reduction's length, as rows
@@ -567,22 +578,24 @@ hipError_t launch_shrink(const AdapterKernelArgs& k, hipStream_t s)
     int ords = 1;
     while (ords < (rows == 16 ? 16 : most) && 2 * ords * blocks <= 2048) ords *= 2;
     auto go = [&](auto kernel, int rt) {
-        EE_LAUNCH(kernel, dim3((unsigned)(blocks * ords), (unsigned)((k.rp + rt * rows - 1) / (rt * rows))), dim3(512), 0, s, k, blocks, ords);
+        EE_LAUNCH(kernel, dim3((unsigned)(blocks * ords), (unsigned)((k.rp + rt * rows - 1) / (rt * rows)), (unsigned)k.splits), dim3(512), 0, s, k, blocks, ords);
         return hipGetLastError();
     };
     if (rows == 16) return k.rp <= 16 ? go(adapter_shrink_kernel<16, 1>, 1) : k.rp <= 32 ? go(adapter_shrink_kernel<16, 2>, 2) : go(adapter_shrink_kernel<16, 4>, 4);
     return k.rp <= 32 ? go(adapter_shrink_kernel<32, 1>, 1) : go(adapter_shrink_kernel<32, 2>, 2);
 }
 
-// Whether the kernel for few rows is the one: up to 32 rows, and where a short reduction over few outputs leaves the tiles little to do or the adapters that may be among a tile's rows lengthen
-// it by a quarter.  Both launches, us, this kernel / 64 x 64 tiles, eight adapters of rank 16: 4096 -> 4096 16 rows 16.2 / 23.4, 32 rows 19.8 / 24.6, 64 rows 27.8 / 27.1, 128 rows 45 / 28;
-// 2048 -> 8192 32 rows 18.0 / 18.1, 48 rows 25.0 / 18.7; 1024 -> 256 64 rows 11.0 / 13.2, 512 rows 11.4 / 13.4; 2048 -> 1000 64 rows 15.9 / 16.2 (24 adapters: 17 / 28), 256 rows 17.5 / 16.3
+// Whether the kernel for few rows is the one: up to 32 rows; while 64 rows to a workgroup are no more than 128 of these (256, where 64 rows are all); up to 256, where a short reduction leaves the
+// tiles little to do or the adapters that may be among a tile's rows lengthen it by a quarter.  Both launches, us, this kernel / tiles, eight adapters of rank 16: 2048 -> 1000 128 rows 11.8 / 16.1,
+// 256 rows 17.8 / 16.3 (24 adapters 18.7 / 22.1), 512 rows 28 / 17; 4096 -> 4096 32 rows 16.2 / 24.4, 64 rows 24.4 / 26.9, 128 rows 43 / 27; 1024 -> 256 512 rows 9.1 / 13.4, 1024 rows
+// 13.3 / 14.8, 2048 rows 28 / 22
 bool few_rows(const AdapterKernelArgs& k)
 {
-    if (k.rows <= 32) return true;
+    const int64_t groups = (int64_t)((k.rows + 63) / 64) * ((k.co + 15) / 16);
+    if (k.rows <= 32 || groups <= (k.rows <= 64 ? 256 : 128)) return true;
     const int different = std::min(std::min(k.adapters, k.slots), 64 / std::max(1, k.rows / k.slots) + 1);
     const bool short_tiles = k.ci <= 1024 || different * (2 * k.rp + 31) / 32 * 4 >= k.kp / 32;
-    return short_tiles && (int64_t)((k.rows + 63) / 64) * ((k.co + 15) / 16) <= 256;
+    return short_tiles && groups <= 256;
 }
 
 hipError_t launch_few_rows(const AdapterKernelArgs& k, hipStream_t s)
@@ -592,7 +605,10 @@ hipError_t launch_few_rows(const AdapterKernelArgs& k, hipStream_t s)
         EE_LAUNCH(kernel, dim3((unsigned)((k.rows + 16 * mt - 1) / (16 * mt) * gn)), dim3(512), 0, s, k, gn);
         return hipGetLastError();
     };
-    return k.rows <= 16 ? go(adapter_rows_project_kernel<1>, 1) : k.rows <= 32 ? go(adapter_rows_project_kernel<2>, 2) : go(adapter_rows_project_kernel<4>, 4);
+    // As few rows to a workgroup as 256 workgroups allow, as long as there are such rows.  16 / 32 / 64 rows, us: 2048 -> 1000 64 rows 10.0 / 11.1 / 15.4, 128 rows 14.7 / 12.5 / 16.1;
+    // 4096 -> 4096 32 rows 17.6 / 16.8 / 18.7
+    auto fits = [&](int r) { return k.rows <= r || (int64_t)((k.rows + r - 1) / r) * gn <= 256; };
+    return fits(16) ? go(adapter_rows_project_kernel<1>, 1) : fits(32) ? go(adapter_rows_project_kernel<2>, 2) : go(adapter_rows_project_kernel<4>, 4);
 }
 
 template <int MB, int NB, int WM, int WN, int KG, int RING, bool F32>
@@ -634,7 +650,7 @@ hipError_t pack(const void* src, int64_t ld, int rows, int cols, void* dst, int6
 int64_t adapter_weight_bytes(const AdapterDims& d) { const AdapterSizes z(d); return z.w + z.bias + 256; }
 int64_t adapter_pool_bytes(const AdapterDims& d) { const AdapterSizes z(d); return std::max<int64_t>(256, z.a + z.b + z.scale); }
 // u | adapters of the rows | a padded copy of x where its rows are no whole 16-byte pieces
-int64_t adapter_workspace(const AdapterDims& d, int64_t rows) { const AdapterSizes z(d); return up(6 * rows * z.rp, 256) + up(4 * rows, 256) + (rows * z.kp * 2); }
+int64_t adapter_workspace(const AdapterDims& d, int64_t rows) { const AdapterSizes z(d); return up(u_bytes(rows) * rows * z.rp, 256) + up(4 * rows, 256) + (rows * z.kp * 2); }
 
 hipError_t launch_adapter_pack(const AdapterDims& d, const void* w, int64_t ldw, const float* bias, void* packed, hipStream_t s)
 {
@@ -666,8 +682,9 @@ hipError_t launch_adapter_project(const AdapterDims& d, const AdapterCall& c, hi
     k.a = (const uint16_t*)c.pool; k.b = (const uint16_t*)((const char*)c.pool + z.a); k.scale = (const float*)((const char*)c.pool + z.a + z.b);
     k.ids = c.ids; k.offsets = c.offsets; k.rows = c.rows; k.slots = c.slots; k.per = c.per;
     k.ci = d.ci; k.co = d.co; k.kp = (int)z.kp; k.np = (int)z.np; k.rp = (int)z.rp; k.ra = (int)z.ra; k.adapters = d.adapters; k.parts = few_rows(k) ? 0 : c.out_f32 ? 3 : 2;
+    k.splits = splits_of(k);
     char* ws = (char*)c.workspace;
-    k.u = (uint16_t*)ws; ws += up(6ll * c.rows * z.rp, 256);
+    k.u = (uint16_t*)ws; ws += up(u_bytes(c.rows) * c.rows * z.rp, 256);
     k.row_ids = (int*)ws; ws += up(4ll * c.rows, 256);
     if (((uintptr_t)c.x & 15) || c.ldx % 8 || d.ci % 8 || c.ldx > 1 << 21) {
         EE_LAUNCH(adapter_rows_kernel, dim3((unsigned)(((int64_t)c.rows * z.kp + 255) / 256)), dim3(256), 0, s, k.x, k.ldx, c.rows, d.ci, (uint16_t*)ws, k.kp);
