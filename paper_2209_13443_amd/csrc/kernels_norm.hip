@@ -4,7 +4,7 @@
 //   bf16  y = act(weight_c (x - mean) / sqrt(var + eps) + bias_c + res), one rounding at the end
 //   int8  S1 = sum x, S2 = sum x^2 (exact integers), d = n x - S1, m_c = weight_c 2^f / (n sqrt((n S2 - S1^2) / n^2 + eps)),
 //         y = clamp(floor(d m_c + (bias_c 2^f + 1/2) + res 2^rs), lo, hi) in 64-bit floats: d is exact, so a constant group gives its bias on
-//         every machine and the results are whole numbers that do not depend on the order of a sum
+//         every machine and the results are whole numbers that do not depend on the order of a sum; every operation is rounded by itself
 // Statistics of bf16: every lane adds up the differences of its values from one of them, and their squares, has from those its own mean and sum of squared differences from it, and such
 // pairs are merged
 // (n = na + nb, delta = mb - ma: mean = ma + delta nb / n, M2 = M2a + M2b + delta^2 na nb / n), so that a mean far from zero costs nothing.
@@ -151,14 +151,14 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
     const int slices = NT / max(64, cols);
     float* const l_n = (float*)lds;                                                                  // bf16: values of the lanes of a slice and column
     pair_t* const l_part = (pair_t*)(lds + (ES == 2 ? 4 * slices * cols : 0));                       // [slice][column][GPV]
-    unsigned char* const l_group = (unsigned char*)(l_part + slices * cols * GPV);                   // per group: bf16 mean and 1 / deviation; int8 S1 and 1 / (n deviation)
+    unsigned char* const l_group = (unsigned char*)(l_part + slices * cols * GPV);                   // per group: bf16 mean and 1 / deviation; int8 S1 and n deviation
     const double n_all = (double)a.pixels * a.cpg;
     auto settle = [&](int g, const stat_t& s) {
         if constexpr (ES == 2) ((float2*)l_group)[g] = float2{s.mean, rsqrtf(s.m2 / (float)n_all + a.eps)};
         else {
             const long long n = (long long)a.pixels * a.cpg;
             const double var = (double)(n * s.s2 - (long long)s.s1 * s.s1) / (n_all * n_all);
-            ((double2*)l_group)[g] = double2{(double)s.s1, 1.0 / (n_all * sqrt(var + (double)a.eps))};
+            ((double2*)l_group)[g] = double2{(double)s.s1, n_all * sqrt(var + (double)a.eps)};
         }
     };
     // every group of the window, 2^sl lanes each that take its `entries` in turn: s = sum of get(group, entry); then f(group, s) in one lane
@@ -412,9 +412,11 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
     } else {
         auto group_of = [&](int e) { return ((const double2*)l_group)[min((col * VEC + e) / a.cpg, wgroups - 1)]; };
         // per channel, in 64 bits: factor, offset
-        auto channel = [&](float w, float bi, double2 g) { return double2{(double)w * a.out_scale * g.y, (double)bi * a.out_scale + 0.5}; };
-        auto in_64 = [&](int v, int r, double s1, double2 c) {       // the definition
-            double t = fma(n_all * v - s1, c.x, c.y);
+        auto channel = [&](float w, float bi, double2 g) { return double2{(double)w * a.out_scale / g.y, (double)bi * a.out_scale + 0.5}; };
+        auto in_64 = [&](int v, int r, double s1, double2 c) {       // the definition, each operation rounded by itself: products that lie halfway between whole numbers are ordinary (n deviation is whole for a group of two values)
+#pragma clang fp contract(off)
+            double t = (n_all * v - s1) * c.x;
+            t += c.y;
             if (has_res) t += r * a.res_scale;
             return (int)fmin(fmax(floor(t), (double)a.lo), (double)a.hi);
         };

@@ -526,3 +526,24 @@ def test_operators_on_another_stream_and_in_graphs(torch, ee):
         for got, want in zip(outs, eager):
             for a, b in zip(got, want):
                 assert torch.equal(a, b), f"turn {turn}"
+
+
+@pytest.mark.parametrize("c,groups", [(32, 16), (64, 8), (6, 3), (10, 2)])
+def test_group_norm_int8_products_between_whole_numbers(torch, ee, c, groups):
+    """Two values a group, without eps: the deviation is a whole number over n, and factors of a quarter put products on halves, where a product that is not rounded before it is added, or a
+    reciprocal in the place of a division, ends one lower."""
+    cpg = c // groups
+    for pixels in (1, 2, 4, 5, 12):
+        n = pixels * cpg
+        x = torch.zeros(20 * (n - 1), n, dtype=torch.int8, device="cuda")
+        w = torch.tensor([0.25, 0.5, 0.75, 1.0, 1.5, 2.0, 2.5, 3.0], device="cuda").repeat((c + 7) // 8)[:c].contiguous()
+        for ones in range(1, n):
+            for i, v in enumerate((1, 2, 3, 5, 7)):
+                for turn in range(4):
+                    x[20 * (ones - 1) + 4 * i + turn, torch.arange(ones, device="cuda").add(turn * 3).remainder(n)] = v
+        x = x.view(-1, pixels, 1, cpg).expand(-1, pixels, groups, cpg).reshape(-1, pixels, c).contiguous()
+        for f in (0, 2, 5):
+            say(f"[case] {c} channels {groups} groups {pixels} pixels frac_bits {f}")
+            ref = norm_ref(torch, x.cpu(), groups, w.cpu(), None, 0.0, "none", None, f)[0].cuda()      # on the CPU, where a division by a number is one
+            got = ee.group_norm(x, groups, w, None, eps=0.0, frac_bits=f)
+            assert torch.equal(got, ref), f"{(got != ref).sum().item()} of {ref.numel()} differ"
