@@ -1,5 +1,5 @@
 // The C ABI of the operators that need no context: argument checks in front of their launches.
-#include "ee_internal.hpp"
+#include "../ee_internal.hpp"
 
 using namespace ee;
 

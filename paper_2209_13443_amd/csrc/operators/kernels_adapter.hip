@@ -10,8 +10,8 @@
 // 8 (l / 32) .. + 7.  A wavefront reads its block as one contiguous KiB per step.  Rows and columns are padded with zeros.
 #include <algorithm>
 
-#include "ee_internal.hpp"
-#include "igemm_device.hpp"
+#include "../ee_internal.hpp"
+#include "../igemm_device.hpp"
 
 namespace ee {
 namespace {

@@ -16,8 +16,8 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "ee_internal.hpp"
-#include "igemm_device.hpp"
+#include "../ee_internal.hpp"
+#include "../igemm_device.hpp"
 
 namespace ee {
 namespace {

@@ -8,8 +8,8 @@
 // that a few sequences fill the chip: the first launch sums the chunks, the second finds the chunk in which the number lies and looks inside.  One chunk: one launch.
 #include <algorithm>
 
-#include "ee_internal.hpp"
-#include "igemm_device.hpp"
+#include "../ee_internal.hpp"
+#include "../igemm_device.hpp"
 
 namespace ee {
 namespace {
