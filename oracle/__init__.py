@@ -200,6 +200,22 @@ def maxpool_bf16(x, k, stride, pad):
     return y
 
 
+def groupnorm(x, groups, weight, bias, eps, act=0, frac_bits=0, res=None, res_shift=0):
+    """x [n, ..., c] int8, or uint16 (bf16 bits)."""
+    i8 = x.dtype == np.int8
+    x = np.ascontiguousarray(x)
+    res = None if res is None else np.ascontiguousarray(res, dtype=x.dtype)
+    weight, bias = _c(weight, np.float32), _c(bias, np.float32)
+    n, c = x.shape[0], x.shape[-1]
+    y = np.empty_like(x)
+    pixels = C.c_int64(int(np.prod(x.shape[1:-1])))
+    if i8:
+        _chk(lib().orc_groupnorm_i8(_p(x), n, pixels, c, groups, _p(weight), _p(bias), C.c_float(eps), act, frac_bits, _p(res), res_shift, _p(y)))
+    else:
+        _chk(lib().orc_groupnorm_bf16(_p(x), n, pixels, c, groups, _p(weight), _p(bias), C.c_float(eps), act, _p(res), _p(y)))
+    return y
+
+
 def avgpool_bf16(x, k, stride, pad):
     x = _c(x, np.uint16)
     n, h, w, c = x.shape

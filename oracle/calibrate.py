@@ -27,7 +27,7 @@ import numpy as np
 
 import oracle as O
 import workloads as W
-from workloads.blob import OP_CONV, OP_DWCONV, OP_MAXPOOL, OP_AVGPOOL, DT_I8
+from workloads.blob import OP_CONV, OP_DWCONV, OP_MAXPOOL, OP_AVGPOOL, OP_GROUPNORM, DT_I8
 
 CALIB_DIR = os.path.join(os.path.dirname(os.path.abspath(W.__file__)), "calib")
 
@@ -112,6 +112,9 @@ def calibrate(name, n_cal=None, log=print):
                 y = O.maxpool_i8(src, kh, stride, pad) if is_i8 else O.maxpool_bf16(src, kh, stride, pad)
             elif kind == OP_AVGPOOL:
                 y = O.avgpool_i8(src, kh, stride, pad) if is_i8 else O.avgpool_bf16(src, kh, stride, pad)
+            elif kind == OP_GROUPNORM:                   # its scale is the network's choice, not the data's
+                entry = dict(shift=int(op["shift"]), res_shift=int(op["res_shift"]))
+                y = O.groupnorm(src, int(op["aux"]) & 0xFFFF, wt, bias, float(op["f_lo"]), int(op["aux"]) >> 16, entry["shift"], res, entry["res_shift"])
             elif is_i8:
                 if kind == OP_CONV:
                     acc = O.conv_acc_i8(src, wt.reshape(co, kh, kw, ci), bias, stride, pad, pad_w=pad_w)

@@ -63,6 +63,10 @@ int orc_conv_bf16(const uint16_t* x, int n, int h, int w, int ci, const uint16_t
 int orc_dwconv_bf16(const uint16_t* x, int n, int h, int w, int c, const uint16_t* wt, const float* bias,
                     int kh, int kw, int stride, int pad, float f_lo, float f_hi, uint16_t* y);
 int orc_maxpool_bf16(const uint16_t* x, int n, int h, int w, int c, int k, int stride, int pad, uint16_t* y);
+int orc_groupnorm_i8(const int8_t* x, int n, int64_t pixels, int c, int groups, const float* weight, const float* bias, float eps, int act, int frac_bits,
+                     const int8_t* res, int res_shift, int8_t* y);
+int orc_groupnorm_bf16(const uint16_t* x, int n, int64_t pixels, int c, int groups, const float* weight, const float* bias, float eps, int act,
+                       const uint16_t* res, uint16_t* y);
 int orc_avgpool_bf16(const uint16_t* x, int n, int h, int w, int c, int k, int stride, int pad, uint16_t* y);
 int orc_conv_bf16_hw(const uint16_t* x, int n, int h, int w, int ci, const uint16_t* wt, const float* bias,
                      int co, int kh, int kw, int stride, int pad, int pad_w, const uint16_t* res, float f_lo, float f_hi,

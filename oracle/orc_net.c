@@ -20,7 +20,7 @@ typedef struct { int32_t first_op, n_ops, n_tensors, out_tensor, out_h, out_w, o
 typedef struct {
     int32_t kind, src, dst, res, h_in, w_in, c_in, h_out, w_out, c_out, kh, kw, stride, pad, shift, res_shift, lo, hi;
     float f_lo, f_hi; int64_t w_off, b_off;
-    int32_t pad_w, c_off, c_tot, reserved;   /* columns of padding; the op writes channels [c_off, c_off + c_out) of a c_tot-channel tensor */
+    int32_t pad_w, c_off, c_tot, aux;   /* columns of padding; the op writes channels [c_off, c_off + c_out) of a c_tot-channel tensor; group norm: groups | activation << 16 */
 } blob_op;
 typedef struct {
     int32_t h, w, c, n_cls, gap_shift, frac_bits; float logit_scale, thr; int64_t w_off, b_off; char reserved[16];
@@ -32,7 +32,7 @@ typedef struct {
     const blob_header* hd; const blob_stage* st; const blob_op* op; const blob_exit* ex;
 } net_view;
 
-enum { KIND_CONV = 0, KIND_DWCONV = 1, KIND_MAXPOOL = 2, KIND_AVGPOOL = 3 };
+enum { KIND_CONV = 0, KIND_DWCONV = 1, KIND_MAXPOOL = 2, KIND_AVGPOOL = 3, KIND_GROUPNORM = 4 };
 
 static int view_blob(const void* blob, size_t bytes, net_view* v)
 {
@@ -75,7 +75,7 @@ int orc_blob_check(const void* blob, size_t bytes)
         filled[0] = tc[0];
         for (int k = 0; k < st->n_ops; ++k) {
             const blob_op* o = &v.op[st->first_op + k];
-            if (o->kind < 0 || o->kind > KIND_AVGPOOL) return ORC_ERR_UNSUPPORTED;
+            if (o->kind < 0 || o->kind > KIND_GROUPNORM) return ORC_ERR_UNSUPPORTED;
             if (o->src < 0 || o->src >= st->n_tensors || o->dst < 1 || o->dst >= st->n_tensors || o->dst == o->src) return ORC_ERR_SHAPE;
             if (filled[o->src] == 0 || filled[o->src] != tc[o->src]) return ORC_ERR_SHAPE;        /* read before it is complete */
             if (o->h_in != th[o->src] || o->w_in != tw[o->src] || o->c_in != tc[o->src]) return ORC_ERR_SHAPE;
@@ -94,8 +94,16 @@ int orc_blob_check(const void* blob, size_t bytes)
             filled[o->dst] += o->c_out;
             if (filled[o->dst] > o->c_tot) return ORC_ERR_SHAPE;
             if (o->res >= 0) {
-                if (o->kind != KIND_CONV || o->res >= st->n_tensors || o->c_tot != o->c_out || filled[o->res] == 0 || filled[o->res] != tc[o->res]) return ORC_ERR_SHAPE;
+                if ((o->kind != KIND_CONV && o->kind != KIND_GROUPNORM) || o->res >= st->n_tensors || o->c_tot != o->c_out || filled[o->res] == 0 || filled[o->res] != tc[o->res]) return ORC_ERR_SHAPE;
                 if (th[o->res] != o->h_out || tw[o->res] != o->w_out || tc[o->res] != o->c_out) return ORC_ERR_SHAPE;
+            }
+            if (o->kind == KIND_GROUPNORM) {
+                const int groups = o->aux & 0xFFFF, act = o->aux >> 16;
+                if (o->kh != 1 || o->stride != 1 || o->pad != 0 || groups < 1 || o->c_in % groups || act < 0 || act > 3 || !(o->f_lo >= 0.f) || o->f_lo > 3.4e38f) return ORC_ERR_SHAPE;
+                if (v.hd->dtype == 0 && (act == 3 || o->shift < 0 || o->shift > 7 || o->res_shift < 0 || o->res_shift > 8 ||
+                                         (int64_t)o->h_in * o->w_in * (o->c_in / groups) >= 1 << 24)) return ORC_ERR_SHAPE;
+                if (o->w_off < v.hd->data_off || (o->w_off & 3) || (size_t)(o->w_off + 4 * (int64_t)o->c_in) > bytes) return ORC_ERR_SHAPE;
+                if (o->b_off < v.hd->data_off || (o->b_off & 3) || (size_t)(o->b_off + 4 * (int64_t)o->c_in) > bytes) return ORC_ERR_SHAPE;
             }
             if (o->kind == KIND_CONV || o->kind == KIND_DWCONV) {
                 const int64_t nw = (int64_t)o->c_out * o->kh * o->kw * (o->kind == KIND_DWCONV ? 1 : o->c_in);
@@ -148,7 +156,15 @@ int orc_stage_forward(const void* blob, size_t bytes, int stage, int b_act, cons
         const void* res = o->res >= 0 ? tens[o->res] : NULL;
         const void* wt = v.base + o->w_off;
         const void* bs = v.base + o->b_off;
-        if (v.hd->dtype == 0) {
+        if (o->kind == KIND_GROUPNORM) {
+            const int64_t pixels = (int64_t)o->h_in * o->w_in;
+            if (v.hd->dtype == 0)
+                rc = orc_groupnorm_i8((const int8_t*)src, b_act, pixels, o->c_in, o->aux & 0xFFFF, (const float*)wt, (const float*)bs, o->f_lo, o->aux >> 16, o->shift,
+                                      (const int8_t*)res, o->res_shift, (int8_t*)dst);
+            else
+                rc = orc_groupnorm_bf16((const uint16_t*)src, b_act, pixels, o->c_in, o->aux & 0xFFFF, (const float*)wt, (const float*)bs, o->f_lo, o->aux >> 16,
+                                        (const uint16_t*)res, (uint16_t*)dst);
+        } else if (v.hd->dtype == 0) {
             if (o->kind == KIND_MAXPOOL) {
                 rc = orc_maxpool_i8((const int8_t*)src, b_act, o->h_in, o->w_in, o->c_in, o->kh, o->stride, o->pad, (int8_t*)dst);
             } else if (o->kind == KIND_AVGPOOL) {

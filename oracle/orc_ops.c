@@ -419,6 +419,75 @@ int orc_avgpool_bf16(const uint16_t* x, int n, int h, int w, int c, int k, int s
     return ORC_OK;
 }
 
+/* Group norm with an activation (0 none, 1 ReLU, 2 ReLU6, 3 SiLU), int8: group g of a sample is c / groups channels of all its pixels, n values with sums S1 and S2 (exact);
+ *   y = clamp(floor((n x - S1) m + (bias 2^f + 1/2) + res 2^rs), lo, hi),  m = weight 2^f / (n sqrt((n S2 - S1^2) / n^2 + eps)),  every operation rounded to double by itself. */
+int orc_groupnorm_i8(const int8_t* x, int n, int64_t pixels, int c, int groups, const float* weight, const float* bias, float eps, int act, int frac_bits,
+                     const int8_t* res, int res_shift, int8_t* y)
+{
+    if (!x || !y || n < 0 || groups < 1 || c % groups || act < 0 || act > 2 || frac_bits < 0 || frac_bits > 7) return ORC_ERR_ARG;
+    const int cpg = c / groups;
+    const int64_t cnt = pixels * cpg;
+    const double unit = ldexp(1.0, frac_bits), rs = ldexp(1.0, res_shift);
+    const double lo = act ? 0.0 : -128.0, hi = act == 2 && 6.0 * unit < 127.0 ? 6.0 * unit : 127.0;
+    for (int b = 0; b < n; ++b)
+        for (int g = 0; g < groups; ++g) {
+            const int64_t base = (int64_t)b * pixels * c + (int64_t)g * cpg;
+            int64_t s1 = 0, s2 = 0;
+            for (int64_t p = 0; p < pixels; ++p)
+                for (int e = 0; e < cpg; ++e) {
+                    const int64_t v = x[base + p * c + e];
+                    s1 += v;
+                    s2 += v * v;
+                }
+            const double var = (double)(cnt * s2 - s1 * s1) / ((double)cnt * (double)cnt), den = (double)cnt * sqrt(var + (double)eps);
+            for (int64_t p = 0; p < pixels; ++p)
+                for (int e = 0; e < cpg; ++e) {
+                    const int64_t at = base + p * c + e;
+                    const double m = (double)weight[g * cpg + e] * unit / den;
+                    double t = (double)(cnt * x[at] - s1) * m;
+                    t = t + ((double)bias[g * cpg + e] * unit + 0.5);
+                    if (res) t = t + (double)res[at] * rs;
+                    t = floor(t);
+                    y[at] = (int8_t)(t > hi ? hi : t > lo ? t : lo);      /* a NaN: lo */
+                }
+        }
+    return ORC_OK;
+}
+
+/* The same, float path: in double, rounded once to float and then to bf16. */
+int orc_groupnorm_bf16(const uint16_t* x, int n, int64_t pixels, int c, int groups, const float* weight, const float* bias, float eps, int act,
+                       const uint16_t* res, uint16_t* y)
+{
+    if (!x || !y || n < 0 || groups < 1 || c % groups || act < 0 || act > 3) return ORC_ERR_ARG;
+    const int cpg = c / groups;
+    const double cnt = (double)pixels * cpg;
+    for (int b = 0; b < n; ++b)
+        for (int g = 0; g < groups; ++g) {
+            const int64_t base = (int64_t)b * pixels * c + (int64_t)g * cpg;
+            double mean = 0.0, var = 0.0;
+            for (int64_t p = 0; p < pixels; ++p)
+                for (int e = 0; e < cpg; ++e) mean += (double)orc_bf16_to_f32(x[base + p * c + e]);
+            mean /= cnt;
+            for (int64_t p = 0; p < pixels; ++p)
+                for (int e = 0; e < cpg; ++e) {
+                    const double d = (double)orc_bf16_to_f32(x[base + p * c + e]) - mean;
+                    var += d * d;
+                }
+            var /= cnt;
+            for (int64_t p = 0; p < pixels; ++p)
+                for (int e = 0; e < cpg; ++e) {
+                    const int64_t at = base + p * c + e;
+                    double t = ((double)orc_bf16_to_f32(x[at]) - mean) / sqrt(var + (double)eps) * (double)weight[g * cpg + e] + (double)bias[g * cpg + e];
+                    if (res) t += (double)orc_bf16_to_f32(res[at]);
+                    if ((act == 1 || act == 2) && t < 0.0) t = 0.0;
+                    if (act == 2 && t > 6.0) t = 6.0;
+                    if (act == 3) t = t / (1.0 + exp(-t));
+                    y[at] = orc_f32_to_bf16((float)t);
+                }
+        }
+    return ORC_OK;
+}
+
 /* Exit head, float path: g_c = mean over pixels (float), z_j = logit_scale * (b_j + sum_c g_c W[j][c]),
  * confidence = softmax top-1 = 1 / sum_j exp(z_j - z_max), label = lowest arg-max. */
 int orc_head_bf16(const uint16_t* x, int n, int h, int w, int c, const uint16_t* wfc, const float* bfc,

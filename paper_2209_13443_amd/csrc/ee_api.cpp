@@ -80,6 +80,22 @@ int pack_op(ee_ctx* ctx, const unsigned char* blob, OpPlan& p)
     }
     const unsigned char* w = blob + d.w_off;
     const unsigned char* b = blob + d.b_off;
+    if (d.kind == OP_GROUPNORM) {
+        p.impl = IMPL_NORM;
+        int rc = upload(ctx, &p.w_dev, std::vector<unsigned char>(w, w + 4 * (size_t)d.c_in));
+        if (!rc) rc = upload(ctx, &p.b_dev, std::vector<unsigned char>(b, b + 4 * (size_t)d.c_in));
+        p.weight_bytes = 8.0 * d.c_in;
+        NormArgs probe = ctx->norm_args(p, 1);
+        probe.y = reinterpret_cast<void*>((uintptr_t)d.c_off * es);  // the slice's place in its pixel, from an aligned tensor
+        if (!rc && !group_norm_supported(probe)) rc = EE_ERR_UNSUPPORTED;
+        if (!rc && (d.c_tot >= 1 << 20 || (((int64_t)d.h_in * d.w_in + 1024) * d.c_tot + d.c_in) * es >= 1ll << 31)) rc = EE_ERR_OVERFLOW;      // the kernel's offsets
+        for (int n = 1; n <= ctx->b_max && !rc; ++n) {               // how a call is cut up depends on the batch
+            const NormArgs a = ctx->norm_args(p, n);
+            if (!group_norm_grid_fits(a)) rc = EE_ERR_OVERFLOW;
+            ctx->norm_ws_bytes = std::max(ctx->norm_ws_bytes, group_norm_workspace(a));
+        }
+        return rc;
+    }
     if (d.kind == OP_DWCONV) {
         if ((d.c_in * es) % 16 != 0 || d.kh != d.kw || d.c_tot != d.c_out) return EE_ERR_UNSUPPORTED;
         p.impl = IMPL_DW;
@@ -597,6 +613,7 @@ int alloc_lane(ee_ctx* ctx, LaneState& L)
     for (int s = 0; s < n_st; ++s)
         if ((rc = dev_alloc(ctx, &L.out_buf[s], (size_t)ctx->stage_out_bytes(s) * b_max))) return rc;
     if ((rc = dev_alloc(ctx, &L.in0, (size_t)ctx->stage_in_bytes(0) * b_max))) return rc;
+    if (ctx->norm_ws_bytes && (rc = dev_alloc(ctx, &L.norm_ws, ctx->norm_ws_bytes))) return rc;
     if ((rc = dev_alloc(ctx, &L.sums, sizeof(int32_t) * (size_t)b_max * ctx->c_max))) return rc;
     if (ctx->c_partial && (rc = dev_alloc(ctx, &L.gap_partial, sizeof(int32_t) * ((size_t)b_max + 1024) * ctx->c_partial))) return rc;
     if ((rc = dev_alloc(ctx, &L.logits, 4 * (size_t)b_max * ctx->net.n_classes))) return rc;
@@ -643,7 +660,7 @@ extern "C" const char* ee_strerror(int status)
 extern "C" const char* ee_kernel_name(int k)
 {
     static const char* names[EE_K_COUNT] = {"conv_mfma", "conv_first", "conv_direct", "depthwise", "maxpool", "pad_input",
-                                            "gap", "fc", "softmax", "compact", "admit", "conv_stream"};
+                                            "gap", "fc", "softmax", "compact", "admit", "conv_stream", "group_norm"};
     return k >= 0 && k < EE_K_COUNT ? names[k] : "?";
 }
 
@@ -693,7 +710,7 @@ extern "C" int ee_create(const void* blob, size_t bytes, int b_max, int dtype, v
         if (std::max(in_rows, out_rows) * es * b_max >= 2147483648.0) return fail(EE_ERR_OVERFLOW);
         const double out_e = (double)d.h_out * d.w_out * d.c_out, in_e = (double)d.h_in * d.w_in * d.c_in;
         const double kred = d.kind == OP_CONV ? (double)d.kh * d.kw * d.c_in : (double)d.kh * d.kw;
-        p.ops_per_sample = d.kind == OP_MAXPOOL || d.kind == OP_AVGPOOL ? 0.0 : 2.0 * out_e * kred;
+        p.ops_per_sample = d.kind == OP_MAXPOOL || d.kind == OP_AVGPOOL || d.kind == OP_GROUPNORM ? 0.0 : 2.0 * out_e * kred;
         p.bytes_per_sample = (in_e + out_e + (d.res >= 0 ? out_e : 0.0)) * es;
         if (p.impl == IMPL_MFMA_C4 || p.impl == IMPL_MFMA_CPAD || p.impl == IMPL_MFMA_S2D) {
             void* pb = nullptr;
@@ -866,7 +883,7 @@ void ee_ctx::bind_lane(int j)
         lanes[(size_t)lane].ids_turn = ids_turn;
     }
     const ee::LaneState& L = lanes[(size_t)j];
-    stream = L.stream; pool = L.pool; pad_bufs = L.pad_bufs; out_buf = L.out_buf; in_buf[0] = L.in0;
+    stream = L.stream; pool = L.pool; pad_bufs = L.pad_bufs; out_buf = L.out_buf; in_buf[0] = L.in0; norm_ws = L.norm_ws;
     sums = L.sums; gap_partial = L.gap_partial; logits = L.logits;
     d_label = L.d_label; d_conf = L.d_conf; d_score = L.d_score; d_flag = L.d_flag; d_slots = L.d_slots;
     h_out = L.h_out; h_ids[0] = L.h_ids[0]; h_ids[1] = L.h_ids[1]; seq = L.seq; head_b = L.head_b; ids_turn = L.ids_turn;
@@ -916,6 +933,17 @@ extern "C" int ee_query(const ee_ctx* ctx, int* n_stages, int64_t* in_bytes, int
         if (out_bytes) out_bytes[s] = ctx->stage_out_bytes(s);
     }
     return EE_OK;
+}
+
+NormArgs ee_ctx::norm_args(const OpPlan& p, int b) const
+{
+    const OpDesc& d = p.d;
+    NormArgs a{};
+    a.dtype = net.dtype; a.act = d.aux >> 16; a.b = b; a.pixels = d.h_in * d.w_in; a.c = d.c_in; a.groups = d.aux & 0xFFFF; a.frac_bits = d.shift; a.res_shift = d.res_shift; a.eps = d.f_lo;
+    a.weight = static_cast<const float*>(p.w_dev); a.bias = static_cast<const float*>(p.b_dev);
+    a.x_pixel = a.res_pixel = d.c_in; a.y_pixel = a.pixels == 1 ? d.c_in : d.c_tot;
+    a.x_sample = a.res_sample = (int64_t)a.pixels * d.c_in; a.y_sample = (int64_t)a.pixels * d.c_tot;
+    return a;
 }
 
 // ---- one convolution on the matrix cores -----------------------------------------------------------
@@ -1812,6 +1840,10 @@ int ee_ctx::run_stage(int stage, int b, const void* act_in, void* act_out, bool 
             DirectConvArgs a{src, p.w_dev, p.b_dev, res, dst, b * d.h_out * d.w_out, d.h_in, d.w_in, d.c_in, d.h_out, d.w_out, d.c_out,
                              d.kh, d.kw, d.stride, d.pad, d.shift, d.res_shift, d.lo, d.hi, d.f_lo, d.f_hi, d.pad_w, d.c_tot, d.c_off};
             e = timed(EE_K_CONV_DIRECT, ops, bytes, [&] { return launch_conv_direct(a, dt, stream); }, st.first_op + k);
+        } else if (p.impl == IMPL_NORM) {
+            NormArgs a = norm_args(p, b);
+            a.x = src; a.res = res; a.y = static_cast<char*>(dst) + (size_t)d.c_off * es;
+            e = timed(EE_K_NORM, ops, bytes, [&] { return launch_group_norm(a, norm_ws, stream); }, st.first_op + k);
         } else {
             PoolArgs a{src, p.w_dev, p.b_dev, dst, p.w3_dev, b, d.h_in, d.w_in, d.c_in, d.h_out, d.w_out, d.kh, d.stride, d.pad, d.shift, d.lo, d.hi, d.f_lo, d.f_hi,
                        d.c_tot, d.c_off};

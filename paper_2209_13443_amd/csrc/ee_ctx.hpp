@@ -7,7 +7,7 @@
 
 namespace ee {
 
-enum Impl { IMPL_MFMA = 0, IMPL_MFMA_C4 = 1, IMPL_DIRECT = 2, IMPL_DW = 3, IMPL_POOL = 4, IMPL_MFMA_CPAD = 5, IMPL_MFMA_S2D = 6, IMPL_AVGPOOL = 7, IMPL_THIN = 8 };
+enum Impl { IMPL_MFMA = 0, IMPL_MFMA_C4 = 1, IMPL_DIRECT = 2, IMPL_DW = 3, IMPL_POOL = 4, IMPL_MFMA_CPAD = 5, IMPL_MFMA_S2D = 6, IMPL_AVGPOOL = 7, IMPL_THIN = 8, IMPL_NORM = 9 };
 enum { BUF_EXT_IN = -1, BUF_EXT_OUT = -2 };
 
 struct OpPlan {
@@ -54,6 +54,7 @@ struct LaneState {
     bool own_stream = false;
     std::vector<void*> pool, pad_bufs, out_buf;
     void* in0 = nullptr;                         // input slots of the first segment
+    void* norm_ws = nullptr;                     // workspace of the group norms
     int32_t* sums = nullptr; int32_t* gap_partial = nullptr; void* logits = nullptr;
     int32_t* d_label = nullptr; float* d_conf = nullptr; int64_t* d_score = nullptr; uint8_t* d_flag = nullptr;
     uint16_t* d_slots = nullptr;                 // the lane's two slot tables (zero-copy compaction)
@@ -119,6 +120,8 @@ struct ee_ctx {
     // lanes of the stream driver: lanes[lane] is a copy of the per-lane members above while that lane is bound
     std::vector<ee::LaneState> lanes;
     int lane = 0;
+    void* norm_ws = nullptr;                     // workspace of the group norms, one behind the other on the lane's stream
+    size_t norm_ws_bytes = 0;                    // what the largest of them needs at any batch size
     std::vector<size_t> pad_buf_bytes;           // size of every padded / folded input copy, for further lanes
     size_t c_max = 0;                            // widest exit head
     size_t c_partial = 0;                        // widest one whose pooling may keep partial rows (0: none does)
@@ -186,6 +189,7 @@ struct ee_ctx {
     // layers op and op + 1 as one fused launch: src feeds layer op, res and dst belong to layer op + 1
     hipError_t launch_pair(int op, int b, const void* src, void* dst, const void* res, int cfg);
     void fill_ir_args(int op, int b, ee::IrArgs& a) const;      // the block headed by layer `op`; x, res and y are left to the caller
+    ee::NormArgs norm_args(const ee::OpPlan& p, int b) const;    // x, res and y are left to the caller
     void fill_conv_args(int op, int b, ee::ConvArgs& a) const;
     static int bucket_of(int b) { int k = 0; while ((1 << k) < b) ++k; return k; }     // smallest k with 2^k >= b
     // to_host: the outcomes also go to h_out, every record with the tag of ++seq (the records are cleared first)

@@ -15,7 +15,7 @@
 namespace ee {
 
 // ---- network description parsed from the blob ------------------------------------------------
-enum OpKind { OP_CONV = 0, OP_DWCONV = 1, OP_MAXPOOL = 2, OP_AVGPOOL = 3 };
+enum OpKind { OP_CONV = 0, OP_DWCONV = 1, OP_MAXPOOL = 2, OP_AVGPOOL = 3, OP_GROUPNORM = 4 };
 
 struct OpDesc {
     int kind, src, dst, res;
@@ -26,6 +26,7 @@ struct OpDesc {
     int64_t w_off, b_off;
     int pad_w;                    // columns of zero padding left and right
     int c_off, c_tot;             // the op writes channels [c_off, c_off + c_out) of a tensor of c_tot channels (concatenation)
+    int aux;                      // group norm: groups | activation << 16 (its epsilon is f_lo)
 };
 
 struct ExitDesc {
@@ -412,7 +413,7 @@ hipError_t launch_compact(const uint8_t* flag, const void* src, void* dst, const
 // Admission: pool rows ids[k] -> slots [0, b)
 hipError_t launch_admit(const void* pool, void* dst, const int32_t* ids, int b, int64_t sample_bytes, hipStream_t s);
 
-// ---- operators that are calls of their own (kernels_norm.hip, kernels_adapter.hip, kernels_verify.hip) -----------------------------
+// ---- operators that are calls of their own (operators/) -----------------------------
 struct NormArgs {         // group norm with an activation; strides in elements, channels are neighbours
     const void* x; const void* res; void* y;
     const float* weight; const float* bias;

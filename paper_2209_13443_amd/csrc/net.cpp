@@ -3,6 +3,8 @@
 // Layout (little endian): 128-byte header, stage records (32 B), op records (112 B), exit records
 // (64 B), then the weight / bias tensors.  Tensor ids are local to a stage: 0 is the stage input; an op
 // writes a new tensor, or a channel slice of a concatenation tensor that other ops fill as well.
+// A group norm is a 1x1 op of stride 1 that keeps its channels: the record's last word holds groups | activation << 16, f_lo the
+// epsilon, shift the fraction bits of an int8 result; its two tensors are float[C] (weight, bias).
 #include <cstring>
 #include <utility>
 
@@ -55,7 +57,7 @@ int parse_blob(const void* blob, size_t bytes, NetDesc* out)
         o.shift = c.next<int32_t>(); o.res_shift = c.next<int32_t>(); o.lo = c.next<int32_t>(); o.hi = c.next<int32_t>();
         o.f_lo = c.next<float>(); o.f_hi = c.next<float>();
         o.w_off = c.next<int64_t>(); o.b_off = c.next<int64_t>();
-        o.pad_w = c.next<int32_t>(); o.c_off = c.next<int32_t>(); o.c_tot = c.next<int32_t>();
+        o.pad_w = c.next<int32_t>(); o.c_off = c.next<int32_t>(); o.c_tot = c.next<int32_t>(); o.aux = c.next<int32_t>();
     }
     net.stages.resize(n_stages);
     net.exits.resize(n_stages);
@@ -76,7 +78,7 @@ int parse_blob(const void* blob, size_t bytes, NetDesc* out)
         th[0] = prev_h; tw[0] = prev_w; tc[0] = prev_c; filled[0] = prev_c;
         for (int k = 0; k < st.n_ops; ++k) {
             const OpDesc& o = net.ops[st.first_op + k];
-            if (o.kind < OP_CONV || o.kind > OP_AVGPOOL) return EE_ERR_UNSUPPORTED;
+            if (o.kind < OP_CONV || o.kind > OP_GROUPNORM) return EE_ERR_UNSUPPORTED;
             if (o.src < 0 || o.src >= st.n_tensors || o.dst < 1 || o.dst >= st.n_tensors || o.dst == o.src) return EE_ERR_SHAPE;
             if (filled[o.src] == 0 || filled[o.src] != tc[o.src]) return EE_ERR_SHAPE;
             if (o.h_in != th[o.src] || o.w_in != tw[o.src] || o.c_in != tc[o.src]) return EE_ERR_SHAPE;
@@ -94,11 +96,19 @@ int parse_blob(const void* blob, size_t bytes, NetDesc* out)
             filled[o.dst] += o.c_out;
             if (filled[o.dst] > o.c_tot) return EE_ERR_SHAPE;
             if (o.res >= 0) {
-                if (o.kind != OP_CONV || o.res >= st.n_tensors || o.c_tot != o.c_out || filled[o.res] == 0 || filled[o.res] != tc[o.res]) return EE_ERR_SHAPE;
+                if ((o.kind != OP_CONV && o.kind != OP_GROUPNORM) || o.res >= st.n_tensors || o.c_tot != o.c_out || filled[o.res] == 0 || filled[o.res] != tc[o.res]) return EE_ERR_SHAPE;
                 if (th[o.res] != ho || tw[o.res] != wo || tc[o.res] != o.c_out) return EE_ERR_SHAPE;
             }
             if (net.dtype == EE_I8 && (o.shift < 0 || o.shift > 30 || o.res_shift < 0 || o.res_shift > 23 || o.lo < -128 || o.hi > 127 || o.lo > o.hi))
                 return EE_ERR_SHAPE;
+            if (o.kind == OP_GROUPNORM) {
+                const int groups = o.aux & 0xFFFF, act = o.aux >> 16;
+                if (o.kh != 1 || o.stride != 1 || o.pad != 0 || groups < 1 || o.c_in % groups != 0 || act < EE_ACT_NONE || act > EE_ACT_SILU) return EE_ERR_SHAPE;
+                if (!(o.f_lo >= 0.f) || !std::isfinite(o.f_lo)) return EE_ERR_SHAPE;
+                if (net.dtype == EE_I8 && (act == EE_ACT_SILU || o.shift > 7 || o.res_shift > 8 || (int64_t)o.h_in * o.w_in * (o.c_in / groups) >= 1 << 24)) return EE_ERR_SHAPE;
+                for (const int64_t off : {o.w_off, o.b_off})
+                    if (off < data_off || off % 4 != 0 || (size_t)(off + 4ll * o.c_in) > bytes) return EE_ERR_SHAPE;
+            }
             if (o.kind == OP_CONV || o.kind == OP_DWCONV) {
                 const int64_t nw = (int64_t)o.c_out * o.kh * o.kw * (o.kind == OP_DWCONV ? 1 : o.c_in);
                 if (o.w_off < data_off || (size_t)(o.w_off + nw * es) > bytes) return EE_ERR_SHAPE;

@@ -16,12 +16,16 @@ slice [c_off, c_off + c_out) of one tensor of c_tot channels (concatenation).
 [C_out][kh][kw][C_in], depthwise weights [C][kh][kw], FC weights [n_cls][C].
 int8 networks carry int8 weights / int32 biases; bf16 networks carry bf16
 weights (raw uint16) / float32 biases.
+
+Group norm (OP_GROUPNORM) is a 1x1 layer of stride 1 that keeps its channels: `aux` is groups | activation << 16
+(0 none, 1 ReLU, 2 ReLU6, 3 SiLU, bf16 only), `f_lo` the epsilon, w_off and b_off float32 [C] of either network type (weight, bias);
+int8: the result is in units of 2^-shift (shift <= 7), the residual enters times 2^res_shift (<= 8).  lo, hi and f_hi are not used.
 """
 import numpy as np
 
 MAGIC = b"EENETv2\0"
 DT_I8, DT_BF16 = 0, 1
-OP_CONV, OP_DWCONV, OP_MAXPOOL, OP_AVGPOOL = 0, 1, 2, 3
+OP_CONV, OP_DWCONV, OP_MAXPOOL, OP_AVGPOOL, OP_GROUPNORM = 0, 1, 2, 3, 4
 
 HEADER_DT = np.dtype([
     ("magic", "S8"), ("version", "<i4"), ("dtype", "<i4"), ("n_stages", "<i4"), ("n_ops", "<i4"),
@@ -45,7 +49,7 @@ OP_DT = np.dtype([
     ("shift", "<i4"), ("res_shift", "<i4"), ("lo", "<i4"), ("hi", "<i4"),
     ("f_lo", "<f4"), ("f_hi", "<f4"),
     ("w_off", "<i8"), ("b_off", "<i8"),
-    ("pad_w", "<i4"), ("c_off", "<i4"), ("c_tot", "<i4"), ("reserved", "<i4"),
+    ("pad_w", "<i4"), ("c_off", "<i4"), ("c_tot", "<i4"), ("aux", "<i4"),
 ])
 assert OP_DT.itemsize == 112
 
@@ -120,6 +124,9 @@ class Blob:
         kind = int(op["kind"])
         if kind in (OP_MAXPOOL, OP_AVGPOOL):
             return None, None
+        if kind == OP_GROUPNORM:
+            c = int(op["c_out"])
+            return tuple(self.raw[int(op[k]):int(op[k]) + 4 * c].view("<f4") for k in ("w_off", "b_off"))
         co, kh, kw, ci = int(op["c_out"]), int(op["kh"]), int(op["kw"]), int(op["c_in"])
         nw = co * kh * kw * (1 if kind == OP_DWCONV else ci)
         return self._tensor(int(op["w_off"]), nw, True), self._tensor(int(op["b_off"]), co, False)

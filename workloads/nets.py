@@ -11,7 +11,7 @@ import numpy as np
 
 from . import rng
 from .blob import (HEADER_DT, STAGE_DT, OP_DT, EXIT_DT, MAGIC, DT_I8, DT_BF16, OP_CONV, OP_DWCONV,
-                   OP_MAXPOOL, OP_AVGPOOL, Blob, f32_to_bf16_bits)
+                   OP_MAXPOOL, OP_AVGPOOL, OP_GROUPNORM, Blob, f32_to_bf16_bits)
 
 BASE_SEED = 0x220913443000
 RELU6_Q = 96  # int8 stand-in for the ReLU6 ceiling (per-tensor power-of-two scales carry no absolute unit)
@@ -97,6 +97,15 @@ class _Net:
 
     def avgpool(self, src, k, stride, pad, into=None):
         return self._pool(OP_AVGPOOL, src, k, stride, pad, into)
+
+    def groupnorm(self, src, groups, act="none", res=-1, into=None, eps=1e-5, frac_bits=5, res_shift=0):
+        """Group norm with an activation ("none", "relu", "relu6", "silu"); the residual is added in front of it.  int8: results in units of 2^-frac_bits."""
+        h, w, c = self._cur["shapes"][src]
+        dst, c_off, c_tot = self._dst((h, w, c), into)
+        self._cur["ops"].append(dict(kind=OP_GROUPNORM, src=src, dst=dst, res=res, h_in=h, w_in=w, c_in=c, h_out=h, w_out=w, c_out=c, kh=1, kw=1, stride=1, pad=0, pad_w=0,
+                                     c_off=c_off, c_tot=c_tot, lo=-128, hi=127, f_lo=eps, f_hi=math.inf, aux=groups | ["none", "relu", "relu6", "silu"].index(act) << 16,
+                                     shift=frac_bits, res_shift=res_shift))
+        return dst
 
 
 # ---------------------------------------------------------------------------
@@ -422,6 +431,35 @@ def single_layer_net(kind, h, w, c, k, stride, pad, dtype, seed=0, co=None, act=
     return blob
 
 
+def norm_net(h, w, ci, groups, dtype, seed=0, mid=64):
+    """Two segments with group norms where networks have them: behind a convolution, with a ReLU; in front of the residual's sum (the norm adds it); of a concatenation, and writing a slice of one;
+    at a segment's border (the first segment ends with one, the second starts with one).  bf16: SiLU in the second.  Data only."""
+    net = _Net(dtype, h, w, ci, 10)
+    t = net.begin_stage()
+    t = net.groupnorm(net.conv(t, mid, 3, 1, 1, act="linear"), groups, "relu")
+    u = net.groupnorm(net.conv(t, mid, 3, 1, 1, act="linear"), groups, "relu6")
+    t = net.groupnorm(net.conv(u, mid, 1, 1, 0, act="linear"), groups, "relu", res=t)
+    net.end_stage(t)
+    t = net.begin_stage()
+    act = "relu" if dtype == DT_I8 else "silu"
+    u = net.groupnorm(t, groups, act)
+    cat = net.new_concat(h, w, 2 * mid + 32)
+    net.groupnorm(t, 1, act, into=(cat, 32))
+    net.conv(u, 32, 1, 1, 0, into=(cat, 0))
+    net.maxpool(u, 3, 1, 1, into=(cat, 32 + mid))
+    v = net.groupnorm(cat, 4, "none", eps=1e-3, frac_bits=4)
+    t = net.groupnorm(net.conv(v, 96, 3, 2, 1, act="linear"), 3, "relu")
+    net.end_stage(t)
+    blob = _assemble(net, dtype, BASE_SEED + 0x7e00 + seed)
+    for op in blob.ops:
+        if int(op["kind"]) == OP_CONV:
+            fan_in = int(op["c_in"]) * int(op["kh"]) * int(op["kw"])
+            op["shift"] = max(0, int(math.ceil(math.log2(2.0 * 74 * 40 * math.sqrt(fan_in) / 127))))
+    for e in blob.exits:
+        e["frac_bits"], e["thr"] = 10, 0.5
+    return blob
+
+
 def inverted_residual_net(h, w, ci, ce, co, stride, seed=0, blocks=1):
     """One segment of `blocks` inverted-residual blocks (1x1 expansion to `ce` channels -- none when ce = 0 --, 3x3 depthwise with the given stride
     in the first block, 1x1 projection to `co` channels (an int, or one value per block), with the block's input as residual where shapes allow) on an
@@ -588,7 +626,8 @@ def _assemble(net, dtype, seed):
             rec = ops[oi]
             for k, v in op.items():
                 rec[k] = v
-            rec["shift"], rec["res_shift"] = 0, 0
+            if op["kind"] != OP_GROUPNORM:
+                rec["shift"], rec["res_shift"] = 0, 0
             if op["kind"] == OP_CONV:
                 kred = op["kh"] * op["kw"] * op["c_in"]
                 rec["w_off"] = put(weights(op["c_out"] * kred, kred))
@@ -597,6 +636,10 @@ def _assemble(net, dtype, seed):
                 kred = op["kh"] * op["kw"]
                 rec["w_off"] = put(weights(op["c_out"] * kred, kred))
                 rec["b_off"] = put(bias(op["c_out"], kred))
+            elif op["kind"] == OP_GROUPNORM:
+                stream += 2
+                rec["w_off"] = put((1.0 + 0.25 * rng.normal_f64(seed, stream - 1, op["c_out"])).astype(np.float32))
+                rec["b_off"] = put((0.25 * rng.normal_f64(seed, stream, op["c_out"])).astype(np.float32))
             oi += 1
         e = exits[s]
         e["h"], e["w"], e["c"], e["n_cls"] = oh, ow, oc, net.n_classes
