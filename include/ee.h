@@ -354,6 +354,7 @@ int ee_group_norm(const ee_norm_desc* desc, const void* x, const float* weight, 
 /* A shared projection with each request's low-rank adapter beside it (bf16): for every row m of x, with a the adapter of its slot,
  *   y[m][o] = sum_c x[m][c] w[o][c] + bias[o] + scale_a sum_r b_a[o][r] (sum_c a_a[r][c] x[m][c])
  * Sums are in float; the inner one is rounded to 2^-18 relative for bf16 results, to 2^-24 for float ones.  y is bf16 or float.
+ * Infinities and NaN of an adapter or of a row of x reach the rows of that adapter, that row, and no others.
  * Weights are laid out once: ee_adapter_bytes sizes the two device buffers (256-byte aligned) a program keeps, ee_adapter_pack fills the first with w[co][ci] and bias (float[co] or
  * NULL), ee_adapter_load puts adapter i (a[rank][ci], b[co][rank], rank <= dims->rank) into the second, also between calls; rank 0 takes it out again (a, b may be NULL).  The second buffer
  * must be zero before its first use (then no adapter adds anything).

@@ -4,7 +4,8 @@
 //
 // Two launches.  The first computes u (adapter_shrink_kernel) and the adapter of every row; u is kept as the sum of bf16 numbers (head and remainders:
 // two of them, relative error 2^-18, for bf16 results, three, 2^-26, for float ones), so that the second half of an adapter runs on the matrix cores as well; few rows keep it in float.  The second is the projection, with the adapters as
-// further steps of its reduction: for each adapter among a wavefront's rows, the rows of others read zeros.
+// further steps of its reduction: for each adapter among a tile's rows, the rows of others read zeros.  A second half that has infinities or NaN, which zeros times it would give to the rows of
+// others, is no step: its own rows add it element by element.
 //
 // Weights are laid out once as operands of the matrix instructions: blocks of 32 rows x steps of 16 columns, [lane][8]: lane l holds row l % 32, columns
 // 8 (l / 32) .. + 7.  A wavefront reads its block as one contiguous KiB per step.  Rows and columns are padded with zeros.
@@ -20,7 +21,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 
 struct AdapterKernelArgs {
     const uint16_t* x; const uint16_t* w; const float* bias; void* y;
-    const uint16_t* a; const uint16_t* b; const float* scale;        // the adapters: first and second halves, factors
+    const uint16_t* a; const uint16_t* b; const float* scale; const int* info;        // the adapters: first and second halves, factors, 2 rank + whether the second half has infinities or NaN
     const int* ids; const int* offsets; int* row_ids; uint16_t* u;
     const uint16_t* zeros;                                           // 16 readable zero bytes
     int64_t ldx, ldy;
@@ -28,15 +29,24 @@ struct AdapterKernelArgs {
 };
 
 // ---- layouts -----------------------------------------------------------------------------------------------------------------
-// dst[row block][step][lane][8] of src[rows][cols] (zeros outside), blocks x steps of them
-__global__ __launch_bounds__(256) void adapter_pack_kernel(const uint16_t* src, int64_t ld, int rows, int cols, uint16_t* dst, int blocks, int steps)
+enum { ODD = 1 << 30 };              // in the adapter of a row: its second half has infinities or NaN
+
+// dst[row block][step][lane][8] of src[rows][cols] (zeros outside), blocks x steps of them.  *info becomes 2 rank; where that has been done (mark) its last bit is set if an element is not finite
+__global__ __launch_bounds__(256) void adapter_pack_kernel(const uint16_t* src, int64_t ld, int rows, int cols, uint16_t* dst, int blocks, int steps, int* info, int rank, bool mark)
 {
+    if (info && !mark && blockIdx.x == 0 && threadIdx.x == 0) *info = 2 * rank;
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;                 // one 16-byte piece
     if (at >= (int64_t)blocks * steps * 64) return;
     const int lane = (int)(at & 63), row = (int)(at / (64 * (int64_t)steps)) * 32 + (lane & 31), col = (int)(at / 64 % steps) * 16 + (lane >> 5) * 8;
     uint16_t v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = row < rows && col + e < cols ? src[row * ld + col + e] : (uint16_t)0;
+    if (mark) {
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) odd |= (v[e] & 0x7F80) == 0x7F80;
+        if (odd) *info = 2 * rank + 1;                     // by all that find one
+    }
     v4i o;
     __builtin_memcpy(&o, v, 16);
     *(v4i*)(dst + at * 8) = o;
@@ -106,7 +116,7 @@ __global__ __launch_bounds__(512) void adapter_shrink_kernel(AdapterKernelArgs a
     if (tid < ROWS) {
         const int m = r0 + tid, id = m < a.rows ? adapter_of(a, m, in_lds ? l_off : a.offsets) : -2;
         l_id[tid] = id;
-        if (m < a.rows && ord == 0 && blockIdx.y == 0 && split == 0) a.row_ids[m] = id;
+        if (m < a.rows && ord == 0 && blockIdx.y == 0 && split == 0) a.row_ids[m] = id >= 0 && (a.info[id] & 1) ? id | ODD : id;
     }
     __syncthreads();
     const int id = l_id[frow];
@@ -134,6 +144,7 @@ __global__ __launch_bounds__(512) void adapter_shrink_kernel(AdapterKernelArgs a
             w[t] = a.a + ((int64_t)ad * (a.ra / 32) + r / 32) * steps16 * 512 + (ROWS == 32 ? lane * 8 : (kq >> 1) * 512 + ((kq & 1) * 32 + (r & 16) + frow) * 8);
         }
         const float scale = a.scale[ad];
+        const int rank = a.info[ad] >> 1;
         acc_t acc[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) acc[t] = acc_t{};
@@ -190,14 +201,14 @@ __global__ __launch_bounds__(512) void adapter_shrink_kernel(AdapterKernelArgs a
                     float v = 0.f;
 #pragma unroll
                     for (int q = 0; q < NW; ++q) v += l_sum[q][row][r];
-                    v *= scale;
+                    v = rank0 + t * ROWS + r < rank ? v * scale : 0.f;           // behind the rank a row's infinity times zeros is NaN
                     if (a.parts == 0) ((float*)a.u)[((int64_t)split * a.rows + r0 + row) * a.rp + rank0 + t * ROWS + r] = v;
                     else {
                         uint16_t* const u = a.u + (int64_t)(r0 + row) * a.parts * a.rp + rank0 + t * ROWS + r;
                         for (int p = 0; p < a.parts; ++p) {
                             const __bf16 h = (__bf16)v;
                             u[p * a.rp] = __builtin_bit_cast(uint16_t, h);
-                            v -= (float)h;
+                            v = __builtin_isfinite((float)h) ? v - (float)h : 0.f;
                         }
                     }
                 }
@@ -258,6 +269,7 @@ __global__ __launch_bounds__(512) void adapter_rows_project_kernel(AdapterKernel
     for (int j = 0; j < J; ++j) {
         const int row = (tid >> 4) + 32 * j, m = m0 + row;
         id[j] = row < 16 * MT && m < a.rows ? a.row_ids ? a.row_ids[m] : -1 : -2;
+        if (id[j] >= 0) id[j] &= ~ODD;                     // adapters are taken by row here
         u[j] = (const float*)a.u + (int64_t)m * a.rp + (tid & 15);
         b[j] = a.b + (((int64_t)id[j] * (a.np / 32) + (nb >> 1)) * (a.rp / 16) * 64 + (nb & 1) * 16 + (tid & 15)) * 8;
     }
@@ -393,7 +405,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
     if (wave_all == 0) {
         int mine[BM / 64], n = 0;
 #pragma unroll
-        for (int i = 0; i < BM / 64; ++i) mine[i] = l_ids[64 * i + lane];
+        for (int i = 0; i < BM / 64; ++i) mine[i] = l_ids[64 * i + lane] < ODD ? l_ids[64 * i + lane] : -1;
         for (;;) {
             int ad = -1;
 #pragma unroll
@@ -524,6 +536,21 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
         const int r0 = (wm * MB + i) * 32;
+        if (const int id = l_ids[r0 + frow]; id >= ODD)
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int o = min(first + n * 32 + 8 * (e >> 2) + 4 * hi + (e & 3), a.np - 1);
+                    const uint16_t* const b = a.b + ((int64_t)(id & ~ODD) * blocks + (o >> 5)) * rs * 512 + (o & 31) * 8;
+                    const uint16_t* const u = a.u + (int64_t)(m0 + r0 + frow) * kx;
+#pragma unroll 1
+                    for (int r = 0; r < a.rp; ++r) {
+                        float v = 0.f;
+                        for (int q = a.parts - 1; q >= 0; --q) v += __uint_as_float((uint32_t)u[q * a.rp + r] << 16);
+                        acc[i][n][e] = fmaf(v, __uint_as_float((uint32_t)b[(r >> 4) * 512 + (r >> 3 & 1) * 256 + (r & 7)] << 16), acc[i][n][e]);
+                    }
+                }
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -567,7 +594,7 @@ struct AdapterSizes {       // in bytes; everything a multiple of 256
     {
         kp = up(d.ci, 64); np = up(d.co, 32); rp = up(std::max(d.rank, 1), 16); ra = up(rp, 32);
         w = 2 * np * kp; bias = up(4 * np, 256);
-        a = 2 * ra * kp * d.adapters; b = 2 * np * rp * d.adapters; scale = up(4ll * d.adapters, 256);
+        a = 2 * ra * kp * d.adapters; b = 2 * np * rp * d.adapters; scale = up(8ll * d.adapters, 256);
     }
 };
 
@@ -638,15 +665,15 @@ hipError_t launch_many_rows(const AdapterKernelArgs& k, hipStream_t s)
     return (double)((tiles(256, 256) + 255) / 256) < 0.37 * (double)((tiles(128, 128) + 255) / 256) ? launch_form<4, 2, 2, 4, 1, 4>(k, s) : launch_form<2, 2, 2, 2, 1, 4>(k, s);
 }
 
-hipError_t pack(const void* src, int64_t ld, int rows, int cols, void* dst, int64_t blocks, int64_t steps, hipStream_t s)
+hipError_t pack(const void* src, int64_t ld, int rows, int cols, void* dst, int64_t blocks, int64_t steps, hipStream_t s, int* info = nullptr, int rank = 0, bool mark = false)
 {
-    EE_LAUNCH(adapter_pack_kernel, dim3((unsigned)((blocks * steps * 64 + 255) / 256)), dim3(256), 0, s, (const uint16_t*)src, ld, rows, cols, (uint16_t*)dst, (int)blocks, (int)steps);
+    EE_LAUNCH(adapter_pack_kernel, dim3((unsigned)((blocks * steps * 64 + 255) / 256)), dim3(256), 0, s, (const uint16_t*)src, ld, rows, cols, (uint16_t*)dst, (int)blocks, (int)steps, info, rank, mark);
     return hipGetLastError();
 }
 
 }  // namespace
 
-// packed weights: operands | bias | 256 zero bytes; adapters: first halves | second halves | factors
+// packed weights: operands | bias | 256 zero bytes; adapters: first halves | second halves | factors | ranks
 int64_t adapter_weight_bytes(const AdapterDims& d) { const AdapterSizes z(d); return z.w + z.bias + 256; }
 int64_t adapter_pool_bytes(const AdapterDims& d) { const AdapterSizes z(d); return std::max<int64_t>(256, z.a + z.b + z.scale); }
 // u | adapters of the rows | a padded copy of x where its rows are no whole 16-byte pieces
@@ -666,8 +693,9 @@ hipError_t launch_adapter_load(const AdapterDims& d, int i, int rank, const void
 {
     const AdapterSizes z(d);
     char* const p = (char*)pool;
-    hipError_t e = pack(a, lda, rank, d.ci, p + z.a / d.adapters * i, z.ra / 32, z.kp / 16, s);
-    if (e == hipSuccess) e = pack(b, ldb, d.co, rank, p + z.a + z.b / d.adapters * i, z.np / 32, z.rp / 16, s);
+    int* const info = (int*)(p + z.a + z.b) + d.adapters + i;
+    hipError_t e = pack(a, lda, rank, d.ci, p + z.a / d.adapters * i, z.ra / 32, z.kp / 16, s, info, rank);
+    if (e == hipSuccess) e = pack(b, ldb, d.co, rank, p + z.a + z.b / d.adapters * i, z.np / 32, z.rp / 16, s, info, rank, true);
     if (e != hipSuccess) return e;
     EE_LAUNCH(adapter_scale_kernel, dim3(1), dim3(1), 0, s, (float*)(p + z.a + z.b) + i, scale);
     return hipGetLastError();
@@ -679,7 +707,7 @@ hipError_t launch_adapter_project(const AdapterDims& d, const AdapterCall& c, hi
     AdapterKernelArgs k{};
     k.x = (const uint16_t*)c.x; k.ldx = c.ldx; k.y = c.y; k.ldy = c.ldy; k.out_f32 = c.out_f32;
     k.w = (const uint16_t*)c.packed; k.bias = (const float*)((const char*)c.packed + z.w); k.zeros = (const uint16_t*)((const char*)c.packed + z.w + z.bias);
-    k.a = (const uint16_t*)c.pool; k.b = (const uint16_t*)((const char*)c.pool + z.a); k.scale = (const float*)((const char*)c.pool + z.a + z.b);
+    k.a = (const uint16_t*)c.pool; k.b = (const uint16_t*)((const char*)c.pool + z.a); k.scale = (const float*)((const char*)c.pool + z.a + z.b); k.info = (const int*)k.scale + d.adapters;
     k.ids = c.ids; k.offsets = c.offsets; k.rows = c.rows; k.slots = c.slots; k.per = c.per;
     k.ci = d.ci; k.co = d.co; k.kp = (int)z.kp; k.np = (int)z.np; k.rp = (int)z.rp; k.ra = (int)z.ra; k.adapters = d.adapters; k.parts = few_rows(k) ? 0 : c.out_f32 ? 3 : 2;
     k.splits = splits_of(k);

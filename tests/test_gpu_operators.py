@@ -547,3 +547,55 @@ def test_group_norm_int8_products_between_whole_numbers(torch, ee, c, groups):
             ref = norm_ref(torch, x.cpu(), groups, w.cpu(), None, 0.0, "none", None, f)[0].cuda()      # on the CPU, where a division by a number is one
             got = ee.group_norm(x, groups, w, None, eps=0.0, frac_bits=f)
             assert torch.equal(got, ref), f"{(got != ref).sum().item()} of {ref.numel()} differ"
+
+
+@pytest.mark.parametrize("rows,ci,co", [(9, 72, 40), (40, 264, 1000), (200, 512, 200), (512, 1088, 512), (2048, 1088, 1000), (4096, 1088, 1000), (8192, 1088, 1000), (16384, 1088, 1024)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_adapter_projection_infinities_stay_with_their_rows(torch, ee, rows, ci, co, dtype):
+    """An adapter with infinities and NaN in both halves beside others: rows of other adapters and of none are what the formula says, its own too.  A row of x with
+    an infinity: the formula's infinities and NaN, in that row only."""
+    g = torch.Generator(device="cuda").manual_seed(rows + co)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    say(f"[case] {rows} rows {ci} -> {co} {dtype}")
+    w = (rnd(co, ci) / ci ** 0.5).bfloat16()
+    proj = ee.AdapterProjection(w, None, adapters=4, rank=16)
+    ranks = (16, 1, 5, 16)
+    ab = [((rnd(r, ci) / ci ** 0.5).bfloat16(), (rnd(co, r) / r ** 0.5).bfloat16()) for r in ranks]
+    a0, b0 = ab[0]
+    b0[5, 2], b0[7, 0], b0[co - 1, 15] = float("inf"), float("nan"), -float("inf")
+    ab[3][0][4, 3] = float("nan")                                          # a first half: its rows are NaN throughout
+    for i, (a, b) in enumerate(ab):
+        proj.load(i, a, b, 0.5)
+    ids = torch.randint(-1, 3, (rows,), device="cuda", generator=g, dtype=torch.int32)
+    ids[rows // 2] = 3
+    ids[0], ids[rows - 1] = 0, 1
+    x = rnd(rows, ci).bfloat16()
+    out = {"bf16": torch.bfloat16, "fp32": torch.float32}[dtype]
+    bits = lambda t: t.view(torch.int16 if dtype == "bf16" else torch.int32)
+    got = proj(x, ids, dtype=out)
+    def near(rows_, cols, i):
+        """rows_ of adapter i (-1: none) against 64 bits; the sums are as long as in the other tests"""
+        xd, wd = x[rows_].double(), w.double()[cols].t()
+        ref, size = xd @ wd, xd.abs() @ wd.abs()
+        if i >= 0:
+            a, b = ab[i][0].double().t(), ab[i][1].double()[cols].t()
+            ref, size = ref + 0.5 * (xd @ a) @ b, size + 0.5 * (xd.abs() @ a.abs()) @ b.abs()
+        return ((got[rows_][:, cols].double() - ref).abs() <= EPS[dtype] * ref.abs() + (ci + 64) * F32 * size).all()
+    for i in (-1, 1, 2):
+        assert near(ids == i, list(range(co)), i), i
+    assert got[ids == 3].isnan().all()
+    own = ids == 0
+    sign = torch.sign(x[own].double() @ a0.double().t())
+    assert torch.equal(got[own][:, 5].double(), sign[:, 2] * float("inf")) and got[own][:, 7].isnan().all() and torch.equal(got[own][:, co - 1].double(), -sign[:, 15] * float("inf"))
+    assert near(own, [o for o in range(co) if o not in (5, 7, co - 1)], 0)
+    # the infinity in x: rank 1, so that the formula's sum is not NaN everywhere
+    x2 = x.clone()
+    x2[rows - 1, 3] = float("inf")
+    got2 = proj(x2, ids, dtype=out)
+    assert torch.equal(bits(got2)[:rows - 1], bits(got)[:rows - 1])
+    inf = float("inf")
+    one = torch.sign(w[:, 3].double()) * inf + torch.sign(ab[1][0][0, 3].double()) * inf * torch.sign(ab[1][1][:, 0].double())
+    assert torch.equal(got2[rows - 1].double().nan_to_num(nan=3.0, posinf=1.0, neginf=-1.0), one.nan_to_num(nan=3.0, posinf=1.0, neginf=-1.0))
+    proj.load(0, *(t.nan_to_num(0, 0, 0) for t in ab[0]), 0.5)              # a sound adapter in its place, none in the other's
+    proj.unload(3)
+    assert proj(x, ids, dtype=out).isfinite().all()
