@@ -463,6 +463,8 @@ def _norm_plan(dtype, x, out, residual, weight, bias, groups, eps, act, frac_bit
     if out is not None:
         y = _pixels(*out, "out")
         _need(out[0] == x[0], "out has to have the shape of x")
+        step, step_pixel = abs(y[3]), y[4] if pixels > 1 else c
+        _need(b <= 1 or pixels == 0 or step >= (pixels - 1) * step_pixel + c or c <= step and step_pixel >= (b - 1) * step + c, "the samples of out must not share elements")
     r = (0, 0, 0, 0, 0)
     if residual is not None:
         _need(residual[0] == x[0], "residual has to have the shape of x")
@@ -508,6 +510,7 @@ def _adapter_plan(ci, co, adapters, rank, x, ids, offsets, out):
     if out is not None:
         _need(out[0] == x[0][:-1] + (co,), "out has to have the shape of x with co channels")
         ldy = _rows(*out, "out")[3]
+        _need(b * inner <= 1 or ldy >= co, "the rows of out must not share elements")
     dims, need = AdapterDims(ci, co, adapters, rank), C.c_int64()
     _chk(_lib.ee_adapter_workspace(C.byref(dims), b * inner, C.byref(need)))
     return b * inner, slots, per, ldx, ldy, need.value

@@ -286,7 +286,7 @@ void plan_verify(const VerifyCall& c, VerifyArgs& a)
     while ((c.v + (int64_t)a.chunk - 1) / a.chunk > 256) a.chunk *= 2;
     a.chunks = (int)((c.v + (int64_t)a.chunk - 1) / a.chunk);
     // 8 workgroups a CU are on the chip at once, so more than 2048 only repeat the decision: 256 rows of 50257, 3328 chunks, take 27.5 us with 2048, 28.8 with a chunk each
-    a.per = (int)std::clamp<int64_t>((int64_t)c.b * a.chunks / 2048, 1, 8);
+    a.per = (int)std::clamp<int64_t>((int64_t)c.b * a.chunks / 2048, 1, a.chunks);
 }
 
 }  // namespace

@@ -599,3 +599,66 @@ def test_adapter_projection_infinities_stay_with_their_rows(torch, ee, rows, ci,
     proj.load(0, *(t.nan_to_num(0, 0, 0) for t in ab[0]), 0.5)              # a sound adapter in its place, none in the other's
     proj.unload(3)
     assert proj(x, ids, dtype=out).isfinite().all()
+
+
+@pytest.mark.parametrize("dtype,b,h,c,groups", [("bf16", 301, 56, 128, 32), ("int8", 601, 56, 128, 8), ("bf16", 5, 250, 400, 5), ("bf16", 70001, 1, 64, 4)])
+def test_group_norm_large_batches_in_place(torch, ee, dtype, b, h, c, groups):
+    """Batches that are worked through in parts, results that are written past the caches, y that is x or the residual, as many samples as no part of them divides."""
+    g = torch.Generator(device="cuda").manual_seed(b)
+    shape = (b, h, h, c)
+    if dtype == "int8":
+        x, res = (torch.randint(-128, 128, shape, device="cuda", generator=g, dtype=torch.int8) for _ in range(2))
+    else:
+        x, res = ((torch.randn(shape, device="cuda", generator=g) * 2 + 1).bfloat16() for _ in range(2))
+    w, bias = torch.randn(c, device="cuda", generator=g), torch.randn(c, device="cuda", generator=g)
+    kw = dict(act="relu", frac_bits=4, res_shift=0) if dtype == "int8" else dict(act="relu")
+    say(f"[case] {dtype} {shape}")
+    apart = ee.group_norm(x, groups, w, bias, residual=res, **kw)
+    for first in range(0, b, max(1, b // 7)):
+        part = slice(first, min(b, first + max(1, b // 7)))
+        ref, bound = norm_ref(torch, x[part].reshape(-1, h * h, c), groups, w, bias, 1e-5, "relu", res[part].reshape(-1, h * h, c), 4 if dtype == "int8" else 0)
+        got = apart[part].reshape(ref.shape)
+        assert torch.equal(got, ref) if bound is None else bool(((got.double() - ref).abs() <= bound).all())
+    for target in ("x", "res"):
+        xx, rr = x.clone(), res.clone()
+        out = xx if target == "x" else rr
+        assert ee.group_norm(xx, groups, w, bias, residual=rr, out=out, **kw) is out
+        assert torch.equal(out, apart), target
+        assert torch.equal(rr if target == "x" else xx, res if target == "x" else x)
+
+
+def test_verify_draft_many_sequences_share_their_rows(torch, ee):
+    """As many sequences as chunks are no longer shared out, over one row of probabilities (stride 0)."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    b, v = 40000, 9001
+    p = torch.softmax(torch.randn(1, 2, v, device="cuda", generator=g), -1).expand(b, 2, v)
+    q = torch.softmax(torch.randn(1, 1, v, device="cuda", generator=g), -1).expand(b, 1, v)
+    draft = torch.randint(0, v, (b, 1), device="cuda", generator=g, dtype=torch.int32)
+    u = torch.rand(b, 2, device="cuda", generator=g)
+    accepted, tokens = ee.verify_draft(draft, p, u, draft_probs=q)
+    pd, qd = p[0].double(), q[0, 0].double()
+    x = draft[:, 0].long()
+    ok = u[:, 0].double() * qd[x] < pd[0][x]
+    assert torch.equal(accepted.long(), ok.long()) and 0 < ok.sum() < b
+    for rows, w, first in ((~ok, (pd[0] - qd).clamp(min=0), 0), (ok, pd[1], 1)):
+        cum = w.cpu().cumsum(0)
+        target = u[rows, 1].double().cpu() * cum[-1]
+        want = torch.searchsorted(cum, target, right=True).clamp(max=v - 1)
+        got = tokens[rows, first].long().cpu()
+        near = (cum[got] - target).abs().minimum((cum[got] - w.cpu()[got] - target).abs()) <= v * 2.0 ** -53 * cum[-1]      # sums in another order
+        assert bool(((got == want) | near).all()) and bool((w.cpu()[got] > 0).all())
+    assert torch.equal(tokens[ok, 0], draft[ok, 0]) and bool((tokens[~ok, 1] == -1).all())
+
+
+def test_results_must_not_share_elements(torch, ee):
+    x = torch.ones(4, 3, 8, device="cuda").bfloat16()
+    wide = torch.zeros(4, 3, 8, device="cuda").bfloat16()
+    for out in (wide[:1].expand(4, 3, 8), wide.view(-1).as_strided((4, 3, 8), (8, 8, 1)), wide.view(-1).as_strided((4, 3, 8), (4, 32, 1)), wide.view(-1).as_strided((4, 3, 8), (8, 31, 1))):
+        with pytest.raises(ee.EEError):
+            ee.group_norm(x, 2, out=out)
+    turns = torch.zeros(3, 4, 8, device="cuda").bfloat16().transpose(0, 1)            # the pixels of the samples take turns
+    assert torch.equal(ee.group_norm(x, 2, out=turns), ee.group_norm(x, 2))
+    proj = ee.AdapterProjection(torch.ones(16, 8, device="cuda").bfloat16())
+    for out in (torch.zeros(16, device="cuda").bfloat16().expand(12, 16), torch.zeros(12 * 16, device="cuda").bfloat16().as_strided((12, 16), (8, 1))):
+        with pytest.raises(ee.EEError):
+            proj(x.view(12, 8), out=out)

@@ -104,3 +104,20 @@ def test_verify_draft_refuses(ee):
     assert call(v=(1 << 30) + 1) == ee.EE_ERR_OVERFLOW and call(b=1 << 24) == ee.EE_ERR_OVERFLOW and call(b=1 << 20, k=1 << 10) == ee.EE_ERR_OVERFLOW
     assert call(b=0) == ee.EE_OK
     assert lib.ee_verify_draft(None, None) == ee.EE_ERR_ARG
+
+
+def test_group_norm_refuses_layouts(ee):
+    lib, n = ee.raw(), C.c_int64(-1)
+
+    def both(code, **k):
+        d = norm(ee, **k)
+        assert lib.ee_group_norm_workspace(C.byref(d), C.byref(n)) == code, k
+        if code:
+            assert lib.ee_group_norm(C.byref(d), P, None, None, P, P, P, 1 << 40, None) == code, k
+    for k in [dict(x_pixel=-64), dict(res_pixel=-1), dict(y_pixel=-64), dict(y_pixel=63)]:
+        both(ee.EE_ERR_ARG, **k)
+    for k in [dict(x_pixel=1 << 20), dict(res_pixel=1 << 20), dict(y_pixel=1 << 20), dict(pixels=1 << 22, x_pixel=512), dict(pixels=1 << 22, y_pixel=512)]:
+        both(ee.EE_ERR_OVERFLOW, **k)
+    for k in [dict(y_sample=-49 * 64), dict(y_sample=64, y_pixel=128), dict(b=1, y_sample=0), dict(pixels=1, y_sample=64, y_pixel=0, x_pixel=-5), dict(x_sample=0), dict(x_pixel=0, res_pixel=0),
+              dict(b=0, y_sample=0), dict(pixels=0, y_sample=0)]:
+        both(ee.EE_OK, **k)
