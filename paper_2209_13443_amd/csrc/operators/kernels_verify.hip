@@ -4,8 +4,9 @@
 // drawn: weights w_j = max(p_n(j) - q_n(j), 0) behind a refusal (p_n where those are all zero), p_n where everything was accepted; the first j with
 // w_0 + .. + w_j > u_K (w_0 + .. + w_{V-1}).  Entries that are not finite and positive weigh nothing.  Sums are held in 64 bits and added in one fixed order.
 //
-// Bound by reading two rows of V entries per sequence, of which only the decision above says which (K gathers, made by every workgroup of the first launch).  Rows are cut into chunks so
-// that a few sequences fill the chip: the first launch sums the chunks, the second finds the chunk in which the number lies and looks inside.  One chunk: one launch.
+// Bound by reading two rows of V entries per sequence, of which only the decision above says which (K gathers, which every workgroup of a sequence makes).  Up to 4096 entries a workgroup of 256
+// threads holds the row; a workgroup per sequence of 1024 threads reads longer ones as long as one CU can; else rows are cut into chunks: the first launch sums them, the second finds the chunk in
+// which the number lies and looks inside.
 #include <algorithm>
 
 #include "../ee_internal.hpp"
@@ -16,7 +17,7 @@ namespace {
 
 struct VerifyArgs {
     VerifyCall c;
-    int chunk, chunks, per;          // entries of a chunk (a multiple of 4096), chunks of a row, chunks a workgroup of the first launch sums
+    int chunk, chunks, per;          // entries of a chunk (a multiple of 4096; 512), chunks of a row, chunks a workgroup of the first launch sums (0: no such launch, a workgroup per sequence)
     double* sums;                    // [b][chunks]
 };
 
@@ -65,33 +66,44 @@ __device__ __forceinline__ Rows rows_of(const VerifyCall& c, int b, int n, int d
     return r;
 }
 
+// eight entries as loaded
+template <bool F32> struct Raw8 {
+    typedef float v4f __attribute__((ext_vector_type(4)));
+    v4f a, b;
+    __device__ __forceinline__ void load(const void* base, int64_t at) { a = *(const v4f*)((const float*)base + at); b = *(const v4f*)((const float*)base + at + 4); }
+    __device__ __forceinline__ void get(float (&o)[8]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { o[e] = a[e]; o[4 + e] = b[e]; }
+    }
+};
+template <> struct Raw8<false> {
+    v4i a;
+    __device__ __forceinline__ void load(const void* base, int64_t at) { a = *(const v4i*)((const uint16_t*)base + at); }
+    __device__ __forceinline__ void get(float (&o)[8]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = __uint_as_float(e & 1 ? (uint32_t)a[e >> 1] & 0xFFFF0000u : (uint32_t)a[e >> 1] << 16);
+    }
+};
+
 // entries j .. j + 7 of a row, 0 behind its end (aligned: j is a multiple of 8 and the row starts on 16 bytes)
 template <bool F32>
 __device__ __forceinline__ void load8(const void* base, int64_t row, int j, int v, bool aligned, float (&o)[8])
 {
     if (aligned && j + 8 <= v) {
-        if constexpr (F32) {
-            typedef float v4f __attribute__((ext_vector_type(4)));
-            const v4f a = *(const v4f*)((const float*)base + row + j), b = *(const v4f*)((const float*)base + row + j + 4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { o[e] = a[e]; o[4 + e] = b[e]; }
-        } else {
-            const v4i a = *(const v4i*)((const uint16_t*)base + row + j);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = __uint_as_float(e & 1 ? (uint32_t)a[e >> 1] & 0xFFFF0000u : (uint32_t)a[e >> 1] << 16);
-        }
+        Raw8<F32> raw;
+        raw.load(base, row + j);
+        raw.get(o);
     } else
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = j + e < v ? prob<F32>(base, row + j + e) : 0.f;
 }
 
-// weights of entries j .. j + 7; one that is not finite and positive is 0
-template <bool F32, bool P_ONLY>
-__device__ __forceinline__ void weights8(const VerifyCall& c, const Rows& r, int j, double (&w)[8])
+// weights of entries j .. j + 7, from p alone or from both; one that is not finite and positive is 0
+template <bool P_ONLY>
+__device__ __forceinline__ void weigh(const Rows& r, int j, const float (&p)[8], const float (&q)[8], double (&w)[8])
 {
-    float p[8], q[8];
-    load8<F32>(c.p, r.p, j, c.v, r.aligned, p);
-    if (!P_ONLY && r.minus) load8<F32>(c.q, r.q, j, c.v, r.aligned, q);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         double t = (double)p[e];
@@ -100,6 +112,23 @@ __device__ __forceinline__ void weights8(const VerifyCall& c, const Rows& r, int
         t = fmax(t, 0.0);                                        // a NaN: 0
         w[e] = t < __builtin_inf() ? t : 0.0;
     }
+}
+// their sum where none is infinite and none is the one to skip: half the work of the above (a NaN counts as 0 here too)
+template <bool P_ONLY>
+__device__ __forceinline__ double sum8(const Rows& r, const float (&p)[8], const float (&q)[8])
+{
+    double w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = fmax(!P_ONLY && r.minus ? (double)p[e] - (double)q[e] : (double)p[e], 0.0);
+    return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+}
+template <bool F32, bool P_ONLY>
+__device__ __forceinline__ void weights8(const VerifyCall& c, const Rows& r, int j, double (&w)[8])
+{
+    float p[8], q[8];
+    load8<F32>(c.p, r.p, j, c.v, r.aligned, p);
+    if (!P_ONLY && r.minus) load8<F32>(c.q, r.q, j, c.v, r.aligned, q);
+    weigh<P_ONLY>(r, j, p, q, w);
 }
 
 // v of the lane CTRL says (a data-parallel-primitive control word: shifts inside rows of 16 lanes, the last lane of a row to the next rows), 0 where there is none
@@ -121,7 +150,8 @@ __device__ __forceinline__ double wave_scan(double v)
     v += from_lane<0x143, 0xC>(v);       // row_bcast 31: lane 31 to rows 2 and 3
     return v;
 }
-// the same over the threads of the workgroup (256); all: over all of them.  Two uses have a barrier between them
+// the same over the threads of the workgroup (of NW wavefronts); all: over all of them.  Two uses of l have a barrier between them
+template <int NW = 4>
 __device__ __forceinline__ double block_scan(double v, double* l, double& all)
 {
     const int wave = threadIdx.x >> 6;
@@ -130,7 +160,9 @@ __device__ __forceinline__ double block_scan(double v, double* l, double& all)
     __syncthreads();
     double before = 0.0;
     for (int w = 0; w < wave; ++w) before += l[w];
-    all = ((l[0] + l[1]) + l[2]) + l[3];
+    all = l[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) all += l[w];
     return before + v;
 }
 
@@ -279,10 +311,131 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a)
         c.tokens[b * (int64_t)(c.k + 1) + i] = drafts < 0 ? -1 : i < n ? c.draft[b * c.draft_row + i] : i == n ? token : -1;
 }
 
+// A workgroup per sequence, one launch.  Its wavefronts take segments of 512 entries (8 a lane) in turn; their sums are scanned, the segment the number lies in is read once more.  What bounds it is
+// what one CU has under way: 256 KB of two rows take 7 us, 512 KB 27 us on all CUs, at 4.8 TB/s.
+enum { SEGMENTS = 256 };
+template <bool F32>
+__global__ __launch_bounds__(1024) void verify_row_kernel(VerifyArgs a)
+{
+    constexpr int NW = 16, AHEAD = F32 ? 2 : 4;                  // AHEAD: segments whose loads a wavefront has in flight
+    __shared__ int l_n, l_at, l_last;
+    __shared__ double l_segment[SEGMENTS], l_sum[2][NW], l_before;
+    const VerifyCall& c = a.c;
+    request_args<sizeof(VerifyArgs)>();
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int drafts = drafts_of(c, b);
+    const double u = c.u[b * c.u_row + c.k];
+    if (wave == 0) {
+        const int n = accepted<F32>(c, b, drafts, lane);
+        if (lane == 0) {
+            l_n = n;
+            c.accepted[b] = max(n, 0);
+            l_at = 0x7FFFFFFF;
+            l_last = -1;
+        }
+    }
+    __syncthreads();
+    const int n = __builtin_amdgcn_readfirstlane(l_n);
+    int token = -1;
+    if (drafts >= 0) {
+        const Rows r = rows_of<F32>(c, b, n, drafts);
+        auto sums = [&](auto p_tag) {
+            constexpr bool P = decltype(p_tag)::value;
+            auto slow = [&](int k) {
+                double w[8];
+                weights8<F32, P>(c, r, k * 512 + lane * 8, w);
+                return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+            };
+            auto add = [&](int k, double s) {
+                s = wave_scan(s);
+                if (lane == 63) l_segment[k] = s;
+            };
+            for (int k = wave; k < a.chunks; k += NW * AHEAD) {
+                const int last = k + NW * (AHEAD - 1);
+                if (r.aligned && last * 512 + 512 <= c.v && !(!P && r.skip >= k * 512 && r.skip < last * 512 + 512)) {       // whole segments: all loads, then the sums
+                    Raw8<F32> p[AHEAD], q[AHEAD];
+#pragma unroll
+                    for (int e = 0; e < AHEAD; ++e) p[e].load(c.p, r.p + (k + NW * e) * 512 + lane * 8);
+                    if (!P && r.minus)
+#pragma unroll
+                        for (int e = 0; e < AHEAD; ++e) q[e].load(c.q, r.q + (k + NW * e) * 512 + lane * 8);
+#pragma unroll
+                    for (int e = 0; e < AHEAD; ++e) {
+                        float pf[8], qf[8];
+                        p[e].get(pf);
+                        if (!P && r.minus) q[e].get(qf);
+                        double s = sum8<P>(r, pf, qf);
+                        if (!(s < __builtin_inf())) s = slow(k + NW * e);        // an infinite entry among the lane's: they are looked at one by one
+                        add(k + NW * e, s);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                } else
+#pragma unroll 1
+                    for (int e = k; e < min(last + 1, a.chunks); e += NW) add(e, slow(e));
+            }
+        };
+        bool p_only = false;
+        double total, mine, incl;
+        sums(std::false_type{});
+        __syncthreads();
+        mine = tid < a.chunks ? l_segment[tid] : 0.0;
+        incl = block_scan<NW>(mine, l_sum[0], total);
+        if (!(total > 0.0)) {                                    // nothing is left of p without q: p itself
+            p_only = true;
+            sums(std::true_type{});
+            __syncthreads();
+            mine = tid < a.chunks ? l_segment[tid] : 0.0;
+            incl = block_scan<NW>(mine, l_sum[1], total);
+        }
+        const double target = u * total;
+        if (total > 0.0) {
+            if (mine > 0.0 && incl > target) atomicMin(&l_at, tid);
+            if (mine > 0.0) atomicMax(&l_last, tid);
+            __syncthreads();
+            const int at = min(l_at, l_last);                    // behind all sums: the last that can be drawn from
+            if (tid == at) l_before = incl - mine;
+            __syncthreads();
+            if (wave > 0) return;
+            const int j = at * 512 + lane * 8;
+            double w[8];
+            if (p_only) weights8<F32, true>(c, r, j, w);
+            else weights8<F32, false>(c, r, j, w);
+            const double s = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])), to = l_before + wave_scan(s);
+            const unsigned long long past = __ballot(s > 0.0 && to > target), some = __ballot(s > 0.0);
+            const int who = past ? (int)__builtin_ctzll(past) : 63 - (int)__builtin_clzll(some);
+            double cum = to - s;
+            int found = -1, behind = -1;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                cum += w[e];
+                if (w[e] > 0.0) {
+                    behind = j + e;
+                    if (found < 0 && cum > target) found = behind;
+                }
+            }
+            token = __builtin_amdgcn_readlane(found >= 0 ? found : behind, who);       // behind every sum (the number is 1, or by rounding): the last entry that can be drawn
+        }
+    }
+    if (wave > 0) return;
+    for (int i = lane; i <= c.k; i += 64)
+        c.tokens[b * (int64_t)(c.k + 1) + i] = drafts < 0 ? -1 : i < n ? c.draft[b * c.draft_row + i] : i == n ? token : -1;
+}
+
+// Whether a workgroup per sequence is the way: rows that leave it little to do alone, longer ones the more CUs are at work; not for more sequences than CUs, which would wait for a second round.
+// Two launches / one, fp32, us: 64 x 5000 12.0 / 7.3, 64 x 16000 12.3 / 8.8, 64 x 32000 13.2 / 12.4, 64 x 64000 15.8 / 16.0, 16 x 32000 12.3 / 12.2, 16 x 64000 12.9 / 14.8, 128 x 64000
+// 22.9 / 19.1, 256 x 128256 53.7 / 48.4 (bf16 37.5 / 33.0), 300 x 16000 19.4 / 18.3, 300 x 32000 25.2 / 28.4
+bool row_each(const VerifyCall& c) { return c.b <= 256 && c.v <= std::max(24576, 512 * c.b); }
+
 void plan_verify(const VerifyCall& c, VerifyArgs& a)
 {
     a.c = c;
     a.chunk = 4096;
+    if (c.v > a.chunk && row_each(c)) {
+        a.chunk = 512;
+        a.chunks = (c.v + 511) / 512;                            // at most SEGMENTS
+        a.per = 0;
+        return;
+    }
     while ((c.v + (int64_t)a.chunk - 1) / a.chunk > 256) a.chunk *= 2;
     a.chunks = (int)((c.v + (int64_t)a.chunk - 1) / a.chunk);
     // 8 workgroups a CU are on the chip at once, so more than 2048 only repeat the decision: 256 rows of 50257, 3328 chunks, take 27.5 us with 2048, 28.8 with a chunk each
@@ -295,7 +448,7 @@ size_t verify_workspace(const VerifyCall& c)
 {
     VerifyArgs a;
     plan_verify(c, a);
-    return a.chunks > 1 ? (size_t)c.b * a.chunks * sizeof(double) : 0;
+    return a.per && a.chunks > 1 ? (size_t)c.b * a.chunks * sizeof(double) : 0;
 }
 
 hipError_t launch_verify(const VerifyCall& c, void* workspace, hipStream_t s)
@@ -304,6 +457,11 @@ hipError_t launch_verify(const VerifyCall& c, void* workspace, hipStream_t s)
     plan_verify(c, a);
     a.sums = (double*)workspace;
     const dim3 each((unsigned)c.b);
+    if (!a.per) {
+        if (c.f32) EE_LAUNCH(verify_row_kernel<true>, each, dim3(1024), 0, s, a);
+        else EE_LAUNCH(verify_row_kernel<false>, each, dim3(1024), 0, s, a);
+        return hipGetLastError();
+    }
     if (a.chunks == 1) {
         if (c.f32) EE_LAUNCH((verify_pick_kernel<true, true>), each, dim3(256), 0, s, a);
         else EE_LAUNCH((verify_pick_kernel<false, true>), each, dim3(256), 0, s, a);

@@ -662,3 +662,37 @@ def test_results_must_not_share_elements(torch, ee):
     for out in (torch.zeros(16, device="cuda").bfloat16().expand(12, 16), torch.zeros(12 * 16, device="cuda").bfloat16().as_strided((12, 16), (8, 1))):
         with pytest.raises(ee.EEError):
             proj(x.view(12, 8), out=out)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("b,v", [(12, 999), (40, 20001), (70, 35003), (13, 24576), (13, 24577), (12, 60001), (256, 5001), (257, 5000)])
+def test_verify_draft_strange_values_in_every_form(torch, ee, b, v, dtype):
+    """Rows of zeros, NaN and infinities, residuals with nothing in them, single entries at every place of a piece, drafts at the ends, numbers at both ends: on both sides of where one workgroup
+    takes a row and where it is cut up."""
+    kind = torch.float32 if dtype == "fp32" else torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(b + v)
+    k = 2
+    p = torch.softmax(2 * torch.randn(b, k + 1, v, device="cuda", generator=g), -1).to(kind)
+    q = torch.softmax(2 * torch.randn(b, k, v, device="cuda", generator=g), -1).to(kind)
+    draft = torch.randint(0, v, (b, k), device="cuda", generator=g, dtype=torch.int32)
+    u = torch.rand(b, k + 1, device="cuda", generator=g)
+    p[0] = 0
+    p[1] = float("nan")
+    p[2, :, v // 2], p[2, :, v - 1] = float("inf"), float("inf")
+    p[3, :, 7], q[3, :, 9] = float("nan"), -float("inf")
+    q[4] = p[4, :k]                      # nothing is left
+    u[4, :k] = 1.0
+    q[5] = float("inf")
+    draft[6, 0], draft[7, 0] = -1, v
+    u[8, k], u[9, k] = 0.0, 1.0
+    p[10] = 0
+    p[10, :, v - 1] = 0.25
+    draft[11, 0], u[11, 0] = v - 1, 1.0
+    for i in range(12, min(b, 40)):      # a single entry
+        at = [0, 7, 8, 511, 512, 513, 8191, v - 9, v - 8][i % 9] % v
+        p[i] = 0
+        p[i, :, at] = 0.5
+    lengths = torch.randint(-1, k + 1, (b,), device="cuda", generator=g, dtype=torch.int32)
+    for qq in (q, None):
+        check_verify(torch, ee, draft, p, qq, u, None, f"{b} x {v} {dtype} strange {qq is not None}")
+        check_verify(torch, ee, draft, p, qq, u, lengths, f"{b} x {v} {dtype} strange, lengths {qq is not None}")
