@@ -312,7 +312,7 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a)
 }
 
 // A workgroup per sequence, one launch.  Its wavefronts take segments of 512 entries (8 a lane) in turn; their sums are scanned, the segment the number lies in is read once more.  What bounds it is
-// what one CU has under way: 256 KB of two rows take 7 us, 512 KB 27 us on all CUs, at 4.8 TB/s.
+// what one CU has under way: 256 KB of two rows take 6 us, 512 KB 25 us on all CUs at once, at 5.2 TB/s.
 enum { SEGMENTS = 256 };
 template <bool F32>
 __global__ __launch_bounds__(1024) void verify_row_kernel(VerifyArgs a)
@@ -350,28 +350,30 @@ __global__ __launch_bounds__(1024) void verify_row_kernel(VerifyArgs a)
                 s = wave_scan(s);
                 if (lane == 63) l_segment[k] = s;
             };
+            // whole segments: all loads, then the sums; the others entry by entry
+            auto whole = [&](int k) { return r.aligned && k * 512 + 512 <= c.v && !(!P && r.skip >= k * 512 && r.skip < k * 512 + 512); };
             for (int k = wave; k < a.chunks; k += NW * AHEAD) {
-                const int last = k + NW * (AHEAD - 1);
-                if (r.aligned && last * 512 + 512 <= c.v && !(!P && r.skip >= k * 512 && r.skip < last * 512 + 512)) {       // whole segments: all loads, then the sums
-                    Raw8<F32> p[AHEAD], q[AHEAD];
+                Raw8<F32> p[AHEAD], q[AHEAD];
 #pragma unroll
-                    for (int e = 0; e < AHEAD; ++e) p[e].load(c.p, r.p + (k + NW * e) * 512 + lane * 8);
-                    if (!P && r.minus)
+                for (int e = 0; e < AHEAD; ++e)
+                    if (whole(k + NW * e)) {
+                        p[e].load(c.p, r.p + (k + NW * e) * 512 + lane * 8);
+                        if (!P && r.minus) q[e].load(c.q, r.q + (k + NW * e) * 512 + lane * 8);
+                    }
 #pragma unroll
-                        for (int e = 0; e < AHEAD; ++e) q[e].load(c.q, r.q + (k + NW * e) * 512 + lane * 8);
-#pragma unroll
-                    for (int e = 0; e < AHEAD; ++e) {
+                for (int e = 0; e < AHEAD; ++e) {
+                    const int at = k + NW * e;
+                    if (at >= a.chunks) break;
+                    double s = __builtin_inf();
+                    if (whole(at)) {
                         float pf[8], qf[8];
                         p[e].get(pf);
                         if (!P && r.minus) q[e].get(qf);
-                        double s = sum8<P>(r, pf, qf);
-                        if (!(s < __builtin_inf())) s = slow(k + NW * e);        // an infinite entry among the lane's: they are looked at one by one
-                        add(k + NW * e, s);
-                        __builtin_amdgcn_sched_barrier(0);
+                        s = sum8<P>(r, pf, qf);
                     }
-                } else
-#pragma unroll 1
-                    for (int e = k; e < min(last + 1, a.chunks); e += NW) add(e, slow(e));
+                    if (!(s < __builtin_inf())) s = slow(at);                    // also where an entry of the lane's is infinite
+                    add(at, s);
+                }
             }
         };
         bool p_only = false;
@@ -422,8 +424,8 @@ __global__ __launch_bounds__(1024) void verify_row_kernel(VerifyArgs a)
 }
 
 // Whether a workgroup per sequence is the way: rows that leave it little to do alone, longer ones the more CUs are at work; not for more sequences than CUs, which would wait for a second round.
-// Two launches / one, fp32, us: 64 x 5000 12.0 / 7.3, 64 x 16000 12.3 / 8.8, 64 x 32000 13.2 / 12.4, 64 x 64000 15.8 / 16.0, 16 x 32000 12.3 / 12.2, 16 x 64000 12.9 / 14.8, 128 x 64000
-// 22.9 / 19.1, 256 x 128256 53.7 / 48.4 (bf16 37.5 / 33.0), 300 x 16000 19.4 / 18.3, 300 x 32000 25.2 / 28.4
+// Two launches / one, fp32, us: 64 x 5000 12.0 / 6.0, 64 x 16000 12.3 / 8.0, 64 x 32000 13.2 / 11.1, 64 x 64000 15.8 / 16.0, 16 x 32000 12.3 / 12.2, 16 x 64000 12.9 / 14.8, 128 x 64000
+// 22.9 / 18.1, 256 x 128256 53.7 / 45.9 (bf16 37.5 / 30.2), 300 x 16000 19.4 / 18.3, 300 x 32000 25.2 / 28.4
 bool row_each(const VerifyCall& c) { return c.b <= 256 && c.v <= std::max(24576, 512 * c.b); }
 
 void plan_verify(const VerifyCall& c, VerifyArgs& a)
