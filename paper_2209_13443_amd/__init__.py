@@ -414,13 +414,21 @@ def _on(device, f, *args):
             _chk(f(*args, _stream_of(device)))
 
 
-def _tensor(t, name, dtypes, device=None):
-    """t's device index (device: the one it has to be)."""
-    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
-        _need(False, f"{name} has to be a tensor of {' or '.join(str(d) for d in dtypes)}", EE_ERR_UNSUPPORTED)
-    at = t.get_device() if t.is_cuda else -1
-    _need(at >= 0 and (device is None or at == device), "tensors have to be on the GPU, all on the same one")
-    return at
+def _key(t):
+    """All that a call's plan needs to know of a tensor, or of None; device -1: not on a GPU."""
+    if t is None:
+        return None
+    try:
+        return t.shape, t.stride(), t.dtype, t.get_device()
+    except (AttributeError, TypeError):
+        return (), (), None, -1              # not a tensor: _check says so
+
+
+def _check(key, name, dtypes, device=None):
+    """Of _key(t); returns the device's index (device: the one it has to be)."""
+    _need(key is not None and key[2] in dtypes, f"{name} has to be a tensor of {' or '.join(str(d) for d in dtypes)}", EE_ERR_UNSUPPORTED)
+    _need(key[3] >= 0 and (device is None or key[3] == device), "tensors have to be on the GPU, all on the same one")
+    return key[3]
 
 
 def _pixels(shape, stride, name):
@@ -450,47 +458,38 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _layout(t):
-    return None if t is None else (t.shape, t.stride())
-
-
-# What follows from shapes and strides alone is worked out once for each of them: 3 to 5 us of a call.
+# What follows from types, shapes and strides alone, refusals too, is worked out once for each of them: 4 to 7 us of a call.
 
 @functools.lru_cache(maxsize=1024)
-def _norm_plan(dtype, x, out, residual, weight, bias, groups, eps, act, frac_bits, res_shift):
-    b, pixels, c, sample, pixel = _pixels(*x, "x")
+def _norm_plan(x, out, residual, weight, bias, groups, eps, act, frac_bits, res_shift):
+    dev = _check(x, "x", (torch.bfloat16, torch.int8, torch.int16))
+    for t, name, dtype in ((out, "out", x[2]), (residual, "residual", x[2]), (weight, "weight", torch.float32), (bias, "bias", torch.float32)):
+        if t is not None:
+            _check(t, name, (dtype,), dev)
+    b, pixels, c, sample, pixel = _pixels(x[0], x[1], "x")
     y = (b, pixels, c, pixels * c, c)
     if out is not None:
-        y = _pixels(*out, "out")
+        y = _pixels(out[0], out[1], "out")
         _need(out[0] == x[0], "out has to have the shape of x")
         step, step_pixel = abs(y[3]), y[4] if pixels > 1 else c
         _need(b <= 1 or pixels == 0 or step >= (pixels - 1) * step_pixel + c or c <= step and step_pixel >= (b - 1) * step + c, "the samples of out must not share elements")
     r = (0, 0, 0, 0, 0)
     if residual is not None:
         _need(residual[0] == x[0], "residual has to have the shape of x")
-        r = _pixels(*residual, "residual")
+        r = _pixels(residual[0], residual[1], "residual")
     for t, name in ((weight, "weight"), (bias, "bias")):
         _need(t is None or t[0] == (c,) and (c == 1 or t[1] == (1,)), f"{name} has to be dense [channels]")
     _need(act in ACTS, f"act has to be one of {', '.join(ACTS)}")
-    d = NormDesc(EE_I8 if dtype == torch.int8 else EE_BF16, ACTS[act], b, pixels, c, groups, frac_bits, res_shift, eps, 0, sample, pixel, r[3], r[4], y[3], y[4])
+    d = NormDesc(EE_I8 if x[2] == torch.int8 else EE_BF16, ACTS[act], b, pixels, c, groups, frac_bits, res_shift, eps, 0, sample, pixel, r[3], r[4], y[3], y[4])
     need = C.c_int64()
     _chk(_lib.ee_group_norm_workspace(C.byref(d), C.byref(need)))
-    return C.byref(d), need.value
+    return dev, C.byref(d), need.value
 
 
 def group_norm(x, groups, weight=None, bias=None, eps=1e-5, act="none", residual=None, frac_bits=0, res_shift=0, out=None):
     """ee_group_norm: act(group norm of x + residual) on x[b, ..., c] (int8, bfloat16 or int16 holding bf16 bits; any sample stride, one pixel stride, channel slices included).
     weight, bias: float32 [c].  act: "none", "relu", "relu6", "silu" (not int8).  int8: the result is in units of 2^-frac_bits, the residual enters times 2^res_shift."""
-    dev = _tensor(x, "x", (torch.bfloat16, torch.int8, torch.int16))
-    if out is not None:
-        _tensor(out, "out", (x.dtype,), dev)
-    if residual is not None:
-        _tensor(residual, "residual", (x.dtype,), dev)
-    if weight is not None:
-        _tensor(weight, "weight", (torch.float32,), dev)
-    if bias is not None:
-        _tensor(bias, "bias", (torch.float32,), dev)
-    desc, need = _norm_plan(x.dtype, _layout(x), _layout(out), _layout(residual), _layout(weight), _layout(bias), index(groups), float(eps), act, index(frac_bits), index(res_shift))
+    dev, desc, need = _norm_plan(_key(x), _key(out), _key(residual), _key(weight), _key(bias), index(groups), float(eps), act, index(frac_bits), index(res_shift))
     if out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
     ws = _workspace(need, x.device)
@@ -499,17 +498,22 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, act="none", residual
 
 
 @functools.lru_cache(maxsize=1024)
-def _adapter_plan(ci, co, adapters, rank, x, ids, offsets, out):
+def _adapter_plan(dev, ci, co, adapters, rank, dtype, x, ids, offsets, out):
+    _check(x, "x", (torch.bfloat16,), dev)
+    _need(dtype in (torch.bfloat16, torch.float32), "results are bfloat16 or float32", EE_ERR_UNSUPPORTED)
+    for t, name, kind in ((offsets, "offsets", torch.int32), (ids, "ids", torch.int32), (out, "out", dtype)):
+        if t is not None:
+            _check(t, name, (kind,), dev)
     if offsets is not None:
         _need(len(x[0]) == 2 and len(offsets[0]) == 1 and offsets[0][0] >= 1 and (offsets[0][0] == 1 or offsets[1] == (1,)), "offsets go with x [rows, ci]")
-    b, inner, channels, ldx = _rows(*x, "x")
+    b, inner, channels, ldx = _rows(x[0], x[1], "x")
     _need(channels == ci, "x has to have ci channels")
     slots, per = (b, inner) if offsets is None else (offsets[0][0] - 1, 0)
     _need(ids is None or ids[0] == (slots,) and (slots <= 1 or ids[1] == (1,)), "ids has to be dense [slots]")
     ldy = co
     if out is not None:
         _need(out[0] == x[0][:-1] + (co,), "out has to have the shape of x with co channels")
-        ldy = _rows(*out, "out")[3]
+        ldy = _rows(out[0], out[1], "out")[3]
         _need(b * inner <= 1 or ldy >= co, "the rows of out must not share elements")
     dims, need = AdapterDims(ci, co, adapters, rank), C.c_int64()
     _chk(_lib.ee_adapter_workspace(C.byref(dims), b * inner, C.byref(need)))
@@ -521,12 +525,12 @@ class AdapterProjection:
     Room for `adapters` adapters of rank <= `rank`; load() puts one in (also between calls), unload() takes it out."""
 
     def __init__(self, weight, bias=None, adapters=0, rank=16):
-        at = _tensor(weight, "weight", (torch.bfloat16,))
+        at = _check(_key(weight), "weight", (torch.bfloat16,))
         dev = weight.device
         _need(weight.dim() == 2 and weight.stride(1) == 1, "weight has to be [co, ci] with dense rows")
         co, ci = weight.shape
         if bias is not None:
-            _tensor(bias, "bias", (torch.float32,), at)
+            _check(_key(bias), "bias", (torch.float32,), at)
             _need(bias.shape == (co,) and bias.is_contiguous(), "bias has to be dense [co]")
         self.device, self.ci, self.co, self.adapters, self.rank = dev, ci, co, adapters, rank
         self._dims = AdapterDims(ci, co, adapters, rank)
@@ -539,7 +543,7 @@ class AdapterProjection:
     def load(self, i, a, b, scale=1.0):
         """Adapter i becomes scale * b a (a: bfloat16 [r, ci], b: bfloat16 [co, r], r <= rank), for the calls behind this one on its stream."""
         for t, name in ((a, "a"), (b, "b")):
-            _tensor(t, name, (torch.bfloat16,), self.device.index)
+            _check(_key(t), name, (torch.bfloat16,), self.device.index)
             _need(t.dim() == 2 and t.stride(1) == 1 or t.shape[1:] == (1,), f"{name} has to have dense rows")
         r = a.shape[0]
         _need(a.shape == (r, self.ci) and b.shape == (self.co, r), "a has to be [r, ci] and b [co, r]")
@@ -552,15 +556,7 @@ class AdapterProjection:
         """x: bfloat16 [slots, ..., ci] or, with offsets (int32 [slots + 1]), [rows, ci] with the rows of slot s at offsets[s]..offsets[s + 1]; ids: int32 [slots], the adapter of
         every slot, outside [0, adapters): none.  Returns bfloat16 or float32 (dtype) with co in place of ci."""
         dev = self.device.index
-        _tensor(x, "x", (torch.bfloat16,), dev)
-        if offsets is not None:
-            _tensor(offsets, "offsets", (torch.int32,), dev)
-        if ids is not None:
-            _tensor(ids, "ids", (torch.int32,), dev)
-        _need(dtype in (torch.bfloat16, torch.float32), "results are bfloat16 or float32", EE_ERR_UNSUPPORTED)
-        if out is not None:
-            _tensor(out, "out", (dtype,), dev)
-        rows, slots, per, ldx, ldy, need = _adapter_plan(self.ci, self.co, self.adapters, self.rank, _layout(x), _layout(ids), _layout(offsets), _layout(out))
+        rows, slots, per, ldx, ldy, need = _adapter_plan(dev, self.ci, self.co, self.adapters, self.rank, dtype, _key(x), _key(ids), _key(offsets), _key(out))
         if out is None:
             out = torch.empty(x.shape[:-1] + (self.co,), dtype=dtype, device=self.device)
         ws = _workspace(need, self.device)
@@ -572,6 +568,13 @@ class AdapterProjection:
 
 @functools.lru_cache(maxsize=1024)
 def _verify_plan(p, draft, u, q, lengths):
+    dev = _check(p, "target_probs", (torch.float32, torch.bfloat16))
+    _check(draft, "draft", (torch.int32,), dev)
+    _check(u, "u", (torch.float32,), dev)
+    if q is not None:
+        _check(q, "draft_probs", (p[2],), dev)
+    if lengths is not None:
+        _check(lengths, "lengths", (torch.int32,), dev)
     dense = lambda t: t[0][-1] <= 1 or t[1][-1] == 1
     _need(len(draft[0]) == 2 and len(p[0]) == 3, "draft has to be [b, k], target_probs [b, k + 1, v]")
     (b, k), v = draft[0], p[0][2]
@@ -581,20 +584,13 @@ def _verify_plan(p, draft, u, q, lengths):
     _need(lengths is None or lengths[0] == (b,) and (b <= 1 or lengths[1] == (1,)), "lengths has to be dense [b]")
     need = C.c_int64()
     _chk(_lib.ee_verify_workspace(b, k, v, C.byref(need)))
-    return b, k, v, (draft[1][0], u[1][0], p[1][0], p[1][1]) + ((0, 0) if q is None else q[1][:2]), need.value
+    return dev, b, k, v, (draft[1][0], u[1][0], p[1][0], p[1][1]) + ((0, 0) if q is None else q[1][:2]), need.value
 
 
 def verify_draft(draft, target_probs, u, draft_probs=None, lengths=None):
     """ee_verify_draft: (accepted int32 [b], tokens int32 [b, k + 1]) for draft int32 [b, k] against target_probs [b, k + 1, v] (float32 or bfloat16), drawn from draft_probs
     [b, k, v] (same type; None: certain), with the random numbers u float32 [b, k + 1] in [0, 1).  lengths int32 [b]: drafts per sequence, < 0: an empty slot."""
-    at = _tensor(target_probs, "target_probs", (torch.float32, torch.bfloat16))
-    _tensor(draft, "draft", (torch.int32,), at)
-    _tensor(u, "u", (torch.float32,), at)
-    if draft_probs is not None:
-        _tensor(draft_probs, "draft_probs", (target_probs.dtype,), at)
-    if lengths is not None:
-        _tensor(lengths, "lengths", (torch.int32,), at)
-    b, k, v, strides, need = _verify_plan(_layout(target_probs), _layout(draft), _layout(u), _layout(draft_probs), _layout(lengths))
+    at, b, k, v, strides, need = _verify_plan(_key(target_probs), _key(draft), _key(u), _key(draft_probs), _key(lengths))
     dev = target_probs.device
     accepted = torch.empty(b, dtype=torch.int32, device=dev)
     tokens = torch.empty((b, k + 1), dtype=torch.int32, device=dev)
