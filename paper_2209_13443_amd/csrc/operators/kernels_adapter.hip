@@ -612,17 +612,18 @@ hipError_t launch_shrink(const AdapterKernelArgs& k, hipStream_t s)
     return k.rp <= 32 ? go(adapter_shrink_kernel<32, 1>, 1) : go(adapter_shrink_kernel<32, 2>, 2);
 }
 
-// Whether the kernel for few rows is the one: up to 32 rows; while 64 rows to a workgroup are no more than 128 of these (256, where 64 rows are all); up to 256, where a short reduction leaves the
-// tiles little to do or the adapters that may be among a tile's rows lengthen it by a quarter.  Both launches, us, this kernel / tiles, eight adapters of rank 16: 2048 -> 1000 128 rows 11.8 / 16.1,
-// 256 rows 17.8 / 16.3 (24 adapters 18.7 / 22.1), 512 rows 28 / 17; 4096 -> 4096 32 rows 16.2 / 24.4, 64 rows 24.4 / 26.9, 128 rows 43 / 27; 1024 -> 256 512 rows 9.1 / 13.4, 1024 rows
-// 13.3 / 14.8, 2048 rows 28 / 22
+// Whether the kernel for few rows is the one: up to 32 rows; up to 64 where 64 rows to a workgroup are no more than 256 of these; else by what both take, in us, with K the reduction in thousands, G
+// the workgroups in 256s, R the rank in 16s behind the first, S the slabs that the adapters among a tile's 64 rows add.  This kernel 4.5 + 0.7 K + 0.5 R + G (2.4 + 4.3 K + R), tiles (up to 256 of
+// 64 x 64) 8 + 2.8 K + 0.3 S.  Measured, both launches, eight adapters of rank 16, this kernel / tiles: 512 -> 1000 256 rows 9.8 / 12.2, 512 rows 14.5 / 12.3 (24 adapters 16.4 / 19.0); 1024 -> 256
+// 512 rows 9.1 / 13.4, 1024 rows 13.3 / 14.8, 2048 rows 28 / 22; 2048 -> 1000 128 rows 11.8 / 16.1, 256 rows 17.8 / 16.3 (24 adapters 18.7 / 22.1); 4096 -> 1024 128 rows 16.1 / 21.9,
+// 256 rows 27.9 / 25.6; 176 -> 3176 96 rows 10.1 / 11.6, 256 rows 17.3 / 11.8 (rank 64 28.5 / 18.5); 4096 -> 4096 32 rows 16.2 / 24.4, 64 rows 24.4 / 26.9, 128 rows 43 / 27
 bool few_rows(const AdapterKernelArgs& k)
 {
     const int64_t groups = (int64_t)((k.rows + 63) / 64) * ((k.co + 15) / 16);
-    if (k.rows <= 32 || groups <= (k.rows <= 64 ? 256 : 128)) return true;
+    if (k.rows <= 32 || (k.rows <= 64 && groups <= 256)) return true;
     const int different = std::min(std::min(k.adapters, k.slots), 64 / std::max(1, k.rows / k.slots) + 1);
-    const bool short_tiles = k.ci <= 1024 || different * (2 * k.rp + 31) / 32 * 4 >= k.kp / 32;
-    return short_tiles && groups <= 256;
+    const double thousands = k.kp / 1024.0, more = k.rp / 16 - 1, slabs = different * (((k.out_f32 ? 3 : 2) * k.rp + 31) / 32);
+    return groups / 256.0 * (2.4 + 4.3 * thousands + more) < 3.5 + 2.1 * thousands + 0.3 * slabs - 0.5 * more;
 }
 
 hipError_t launch_few_rows(const AdapterKernelArgs& k, hipStream_t s)

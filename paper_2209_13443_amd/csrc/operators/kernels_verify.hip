@@ -52,25 +52,28 @@ __device__ __forceinline__ int accepted(const VerifyCall& c, int b, int drafts, 
 }
 
 // the rows the extra token is drawn from: p, less q (minus) or without one entry (skip)
-struct Rows { int64_t p, q; bool minus, aligned; int skip; };
+struct Rows { int64_t p, q; bool minus; int skip; };
 template <bool F32>
 __device__ __forceinline__ Rows rows_of(const VerifyCall& c, int b, int n, int drafts)
 {
-    Rows r{b * c.p_seq + n * c.p_row, 0, false, false, -1};
+    Rows r{b * c.p_seq + n * c.p_row, 0, false, -1};
     if (n < drafts) {
         if (c.q) { r.minus = true; r.q = b * c.q_seq + n * c.q_row; }
         else r.skip = c.draft[b * c.draft_row + n];
     }
-    constexpr int ES = F32 ? 4 : 2;
-    r.aligned = (((uintptr_t)c.p + r.p * ES) & 15) == 0 && (!r.minus || (((uintptr_t)c.q + r.q * ES) & 15) == 0);
     return r;
 }
 
-// eight entries as loaded
+// eight entries as loaded, from wherever a row starts: 16-byte loads need no alignment
 template <bool F32> struct Raw8 {
     typedef float v4f __attribute__((ext_vector_type(4)));
     v4f a, b;
-    __device__ __forceinline__ void load(const void* base, int64_t at) { a = *(const v4f*)((const float*)base + at); b = *(const v4f*)((const float*)base + at + 4); }
+    __device__ __forceinline__ void load(const void* base, int64_t at)
+    {
+        const float* const p = (const float*)base + at;
+        __builtin_memcpy(&a, p, 16);
+        __builtin_memcpy(&b, p + 4, 16);
+    }
     __device__ __forceinline__ void get(float (&o)[8]) const
     {
 #pragma unroll
@@ -79,7 +82,7 @@ template <bool F32> struct Raw8 {
 };
 template <> struct Raw8<false> {
     v4i a;
-    __device__ __forceinline__ void load(const void* base, int64_t at) { a = *(const v4i*)((const uint16_t*)base + at); }
+    __device__ __forceinline__ void load(const void* base, int64_t at) { __builtin_memcpy(&a, (const uint16_t*)base + at, 16); }
     __device__ __forceinline__ void get(float (&o)[8]) const
     {
 #pragma unroll
@@ -87,11 +90,11 @@ template <> struct Raw8<false> {
     }
 };
 
-// entries j .. j + 7 of a row, 0 behind its end (aligned: j is a multiple of 8 and the row starts on 16 bytes)
+// entries j .. j + 7 of a row, 0 behind its end
 template <bool F32>
-__device__ __forceinline__ void load8(const void* base, int64_t row, int j, int v, bool aligned, float (&o)[8])
+__device__ __forceinline__ void load8(const void* base, int64_t row, int j, int v, float (&o)[8])
 {
-    if (aligned && j + 8 <= v) {
+    if (j + 8 <= v) {
         Raw8<F32> raw;
         raw.load(base, row + j);
         raw.get(o);
@@ -126,8 +129,8 @@ template <bool F32, bool P_ONLY>
 __device__ __forceinline__ void weights8(const VerifyCall& c, const Rows& r, int j, double (&w)[8])
 {
     float p[8], q[8];
-    load8<F32>(c.p, r.p, j, c.v, r.aligned, p);
-    if (!P_ONLY && r.minus) load8<F32>(c.q, r.q, j, c.v, r.aligned, q);
+    load8<F32>(c.p, r.p, j, c.v, p);
+    if (!P_ONLY && r.minus) load8<F32>(c.q, r.q, j, c.v, q);
     weigh<P_ONLY>(r, j, p, q, w);
 }
 
@@ -351,7 +354,7 @@ __global__ __launch_bounds__(1024) void verify_row_kernel(VerifyArgs a)
                 if (lane == 63) l_segment[k] = s;
             };
             // whole segments: all loads, then the sums; the others entry by entry
-            auto whole = [&](int k) { return r.aligned && k * 512 + 512 <= c.v && !(!P && r.skip >= k * 512 && r.skip < k * 512 + 512); };
+            auto whole = [&](int k) { return k * 512 + 512 <= c.v && !(!P && r.skip >= k * 512 && r.skip < k * 512 + 512); };
             for (int k = wave; k < a.chunks; k += NW * AHEAD) {
                 Raw8<F32> p[AHEAD], q[AHEAD];
 #pragma unroll
