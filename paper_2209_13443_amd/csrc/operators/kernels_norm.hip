@@ -135,8 +135,8 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
     using raw = typename P::raw;
     typedef typename std::conditional<ES == 2, Moments, Sums>::type stat_t;
     typedef typename std::conditional<ES == 2, float2, Sums>::type pair_t;
-    constexpr int SUB = VEC / GPV, LOG_NT = NT == 256 ? 8 : 10;
-    static_assert(NT == 256 || NT == 1024);
+    constexpr int SUB = VEC / GPV, LOG_NT = NT == 256 ? 8 : NT == 512 ? 9 : 10;
+    static_assert(NT == 256 || NT == 512 || NT == 1024);
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int u = xcd_unit(blockIdx.x, a.units);
     if (u < 0) return;
@@ -514,25 +514,29 @@ bool plan_norm_vec(const NormArgs& a, int vec, NormPlan& p)
         p.windows = (all + p.wv - 1) / p.wv;
     };
     auto fits = [&] { return (1 << p.wlog) <= p.nt && norm_lds(es, p.gpv, p.nt, p.wlog, p.wv * vec / cpg, p.wv * vec) <= NORM_LDS; };
-    static const int forms[][2] = {{256, 1}, {256, 4}, {1024, 4}};
-    // one launch: 128 bytes of a pixel to a workgroup, or less (down to 32) where that makes too few workgroups or is more than one holds.  int8 64 x 14x14x1024, 64 bytes for 128: 22 -> 15 us
-    bool found = false;
-    for (int want = vec == 1 ? 64 : 8; want >= (vec == 1 ? 16 : 2); want /= 2) {
-        NormPlan t = p;
+    // one launch.  The largest window that 256 threads hold, of at least 128 workgroups if there are such: what a workgroup does before its first result is the same for any.  bf16, columns of 16 bytes
+    // and us: 1000 x 3x3x256 4 29, 8 19, 32 12.4; 512 x 4x4x1024 8 35, 16 34, 64 13.8; 256 x 7x7x512 4 17, 8 14.7, 16 13.4; 78 x 180x128 2 7.5, 4 6.2; 1 x 7x7x2048 8 5.6, 16 6.4
+    const int least = vec == 1 ? 16 : 2;
+    p.chunks = 1;
+    p.chunk_pixels = a.pixels;
+    NormPlan held{};
+    for (int want = 256; want >= least; want /= 2) {
         window(want);
-        for (const auto& f : forms) {
-            p.nt = f[0]; p.nv = f[1];
-            if (!fits() || (int64_t)p.nv * (p.nt >> p.wlog) < a.pixels) continue;
-            p.chunks = 1; p.chunk_pixels = a.pixels;
-            if (found && p.wlog == t.wlog) break;
-            found = true;
-            t = p;
-            break;
-        }
-        p = t;
-        if (found && (int64_t)a.b * p.windows >= 1024) break;
+        p.nt = 256;
+        const int64_t vectors = (int64_t)a.pixels << p.wlog;
+        p.nv = vectors <= 256 ? 1 : 4;
+        if (vectors > 1024 || !fits()) continue;
+        held = p;
+        held.ok = true;
+        if ((int64_t)a.b * p.windows >= 128) break;
     }
-    if (found) return true;
+    if (held.ok) { p = held; return true; }
+    // the smallest window and more threads; 1024 only while all workgroups are at work at once.  This / two launches, bf16, us: 41 x 770x256 13.2 / 15.4, 256 x 900x256 54.8 / 57.0;
+    // 1024 threads 16 x 1600x256 11.8 / 14.3, 64 x 2000x128 23.7 / 19.9, 256 x 1100x64 34 / 21
+    window(least);
+    p.nv = 4;
+    for (p.nt = 512; p.nt <= 1024; p.nt *= 2)
+        if (fits() && (int64_t)a.pixels << p.wlog <= 4 * p.nt && (p.nt == 512 || (int64_t)a.b * p.windows <= 256)) return true;
     // two launches, of whole pixels where they are up to 1 KiB.  Few long workgroups: what one does before its first result is worth tens of KB.  256 / 512 / 1024 / 2048 of them, bf16, us:
     // 64 x 56x56x256 with residual 69, 68, 75, 79, 16 of these 24, 27, 31, 31; 256 x 112x112x64 225, 222, 224, 221
     for (int want = 64; want >= 8; want /= 2) {
@@ -596,7 +600,7 @@ hipError_t launch_norm_gpv(const NormKernelArgs& k, const NormPlan& p, hipStream
         return e == hipSuccess ? launch_norm_form<ES, VEC, GPV, 1024, 4, 2>(k, s) : e;
     }
     if (p.nt == 256) return p.nv == 1 ? launch_norm_form<ES, VEC, GPV, 256, 1, 0>(k, s) : launch_norm_form<ES, VEC, GPV, 256, 4, 0>(k, s);
-    return launch_norm_form<ES, VEC, GPV, 1024, 4, 0>(k, s);
+    return p.nt == 512 ? launch_norm_form<ES, VEC, GPV, 512, 4, 0>(k, s) : launch_norm_form<ES, VEC, GPV, 1024, 4, 0>(k, s);
 }
 
 bool norm_aligned(const NormArgs& a)
