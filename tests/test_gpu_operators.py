@@ -32,6 +32,12 @@ def ee():
 
 
 # ---- group norm -------------------------------------------------------------------------------------------------------------------
+def over(t, f):
+    """f ("sum", "amax") over pixels and a group's channels, the pixels on the CPU: the library's reductions of few results over many workgroups have given wrong ones here now and then (the
+    same call again another value, the operator's result the same)."""
+    return getattr(getattr(t, f)(3, keepdim=True).cpu(), f)(1, keepdim=True).to(t.device)
+
+
 def norm_ref(torch, x, groups, w, b, eps, act, res, f=0, rs=0):
     """(result, bound) in 64 bits; x [b, p, c]"""
     n_b, pix, c = x.shape
@@ -41,7 +47,7 @@ def norm_ref(torch, x, groups, w, b, eps, act, res, f=0, rs=0):
     if x.dtype == torch.int8:
         xi = x.long().view(n_b, pix, groups, cpg)
         n = pix * cpg
-        s1, s2 = xi.sum((1, 3), keepdim=True), (xi * xi).sum((1, 3), keepdim=True)
+        s1, s2 = over(xi, "sum"), over(xi * xi, "sum")
         var = (n * s2 - s1 * s1).double() / float(n) ** 2
         t = (n * xi - s1).double() * (w.view(groups, cpg) * 2.0 ** f / (n * (var + np.float32(eps)).sqrt())) + (b.view(groups, cpg) * 2.0 ** f + 0.5)
         t = t.view(x.shape)
@@ -50,11 +56,11 @@ def norm_ref(torch, x, groups, w, b, eps, act, res, f=0, rs=0):
         lo, hi = {"none": (-128, 127), "relu": (0, 127), "relu6": (0, min(127, 6 * 2 ** f))}[act]
         return t.floor().clamp(lo, hi).to(torch.int8), None
     xd = x.double().view(n_b, pix, groups, cpg)
-    mean = xd.mean((1, 3), keepdim=True)
-    a = w.view(groups, cpg) / ((xd - mean).square().mean((1, 3), keepdim=True) + np.float32(eps)).sqrt()
+    mean = over(xd, "sum") / (pix * cpg)
+    a = w.view(groups, cpg) / (over((xd - mean).square(), "sum") / (pix * cpg) + np.float32(eps)).sqrt()
     y = ((xd - mean) * a + b.view(groups, cpg)).view(x.shape)
     # the mean and the variance from at most a few dozen additions behind one another each, of numbers as large as the largest
-    size = (((xd - mean).abs() + xd.abs().amax((1, 3), keepdim=True)) * a.abs()).view(x.shape) + b.abs()
+    size = (((xd - mean).abs() + over(xd.abs(), "amax")) * a.abs()).view(x.shape) + b.abs()
     if res is not None:
         y = y + res.double()
         size = size + res.double().abs()
@@ -696,3 +702,34 @@ def test_verify_draft_strange_values_in_every_form(torch, ee, b, v, dtype):
     for qq in (q, None):
         check_verify(torch, ee, draft, p, qq, u, None, f"{b} x {v} {dtype} strange {qq is not None}")
         check_verify(torch, ee, draft, p, qq, u, lengths, f"{b} x {v} {dtype} strange, lengths {qq is not None}")
+
+
+def test_group_norm_widest_groups(torch, ee):
+    g = torch.Generator(device="cuda").manual_seed(8)
+    for dtype, c in ((torch.int8, 8192), (torch.bfloat16, 8192), (torch.int8, 4096), (torch.int8, 1023), (torch.bfloat16, 1023)):
+        for pixels in (1, 3, 40):
+            say(f"[case] {dtype} {pixels} x {c}")
+            x = torch.randint(-128, 128, (2, pixels, c), device="cuda", generator=g, dtype=torch.int8).to(dtype)
+            w, b = torch.randn(c, device="cuda", generator=g), torch.randn(c, device="cuda", generator=g)
+            f = 5 if dtype == torch.int8 else 0
+            ref, bound = norm_ref(torch, x, 1, w, b, 1e-5, "none", None, f)
+            got = ee.group_norm(x, 1, w, b, frac_bits=f)
+            assert torch.equal(got, ref) if bound is None else bool(((got.double() - ref).abs() <= bound).all())
+    for dtype, c in ((torch.int8, 8208), (torch.bfloat16, 8200), (torch.int8, 1025), (torch.bfloat16, 1025)):
+        with pytest.raises(ee.EEError) as e:
+            ee.group_norm(torch.zeros(1, 2, c, device="cuda", dtype=dtype), 1)
+        assert e.value.code == ee.EE_ERR_UNSUPPORTED
+
+
+def test_group_norm_int8_values_near_whole_numbers_everywhere(torch, ee):
+    """One factor for all channels and few different values: a value near a whole number is one in all of a group."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    for pixels, c, groups in ((2000, 128, 8), (49, 512, 32), (9, 48, 16), (700, 64, 2)):
+        x = torch.randint(-2, 3, (6, pixels, c), device="cuda", generator=g, dtype=torch.int8)
+        res = torch.randint(-128, 128, x.shape, device="cuda", generator=g, dtype=torch.int8)
+        for scale, f, rs in ((1.0, 0, 0), (0.5, 4, -1), (3.0, 7, -8), (2.0 ** -20, 0, 0)):
+            w, b = torch.full((c,), scale, device="cuda"), torch.full((c,), 2 * scale, device="cuda")
+            for r in (None, res):
+                say(f"[case] {pixels} {c} {groups} scale {scale} f {f} rs {rs} residual {r is not None}")
+                ref, _ = norm_ref(torch, x, groups, w, b, 1e-5, "none", r, f, rs)
+                assert torch.equal(ee.group_norm(x, groups, w, b, frac_bits=f, residual=r, res_shift=rs), ref)
