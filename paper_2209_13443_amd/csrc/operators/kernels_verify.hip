@@ -4,8 +4,8 @@
 // drawn: weights w_j = max(p_n(j) - q_n(j), 0) behind a refusal (p_n where those are all zero), p_n where everything was accepted; the first j with
 // w_0 + .. + w_j > u_K (w_0 + .. + w_{V-1}).  Entries that are not finite and positive weigh nothing.  Sums are held in 64 bits and added in one fixed order.
 //
-// Bound by reading two rows of V entries per sequence, of which only the decision above says which (K gathers, which every workgroup of a sequence makes).  Up to 4096 entries a workgroup of 256
-// threads holds the row; a workgroup per sequence of 1024 threads reads longer ones as long as one CU can; else rows are cut into chunks: the first launch sums them, the second finds the chunk in
+// Bound by reading two rows of V entries per sequence, of which only the decision above says which (K gathers, which every workgroup of a sequence makes).  Short rows are held by a workgroup
+// of 256 threads; one of 1024 threads reads longer ones as long as one CU can; else rows are cut into chunks: the first launch sums them, the second finds the chunk in
 // which the number lies and looks inside.
 #include <algorithm>
 
@@ -100,7 +100,10 @@ __device__ __forceinline__ void load8(const void* base, int64_t row, int j, int 
         raw.get(o);
     } else
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = j + e < v ? prob<F32>(base, row + j + e) : 0.f;
+        for (int e = 0; e < 8; ++e) {
+            const float last = prob<F32>(base, row + min(j + e, v - 1));          // all eight in flight: no branches
+            o[e] = j + e < v ? last : 0.f;
+        }
 }
 
 // weights of entries j .. j + 7, from p alone or from both; one that is not finite and positive is 0
@@ -427,15 +430,15 @@ __global__ __launch_bounds__(1024) void verify_row_kernel(VerifyArgs a)
 }
 
 // Whether a workgroup per sequence is the way: rows that leave it little to do alone, longer ones the more CUs are at work; not for more sequences than CUs, which would wait for a second round.
-// Two launches / one, fp32, us: 64 x 5000 12.0 / 6.0, 64 x 16000 12.3 / 8.0, 64 x 32000 13.2 / 11.1, 64 x 64000 15.8 / 16.0, 16 x 32000 12.3 / 12.2, 16 x 64000 12.9 / 14.8, 128 x 64000
+// The kernel for up to 4096 entries / this, fp32, us: 128 x 256 5.7 / 5.8, 128 x 512 6.7 / 4.9, 128 x 4096 8.7 / 5.2, 512 x 4096 10.0 / 8.3, 512 x 256 6.4 / 9.0.  Two launches / this: 64 x 5000 12.0 / 6.0, 64 x 16000 12.3 / 8.0, 64 x 32000 13.2 / 11.1, 64 x 64000 15.8 / 16.0, 16 x 32000 12.3 / 12.2, 16 x 64000 12.9 / 14.8, 128 x 64000
 // 22.9 / 18.1, 256 x 128256 53.7 / 45.9 (bf16 37.5 / 30.2), 300 x 16000 19.4 / 18.3, 300 x 32000 25.2 / 28.4
-bool row_each(const VerifyCall& c) { return c.b <= 256 && c.v <= std::max(24576, 512 * c.b); }
+bool row_each(const VerifyCall& c) { return c.b <= 256 && c.v >= 512 && c.v <= std::max(24576, 512 * c.b); }
 
 void plan_verify(const VerifyCall& c, VerifyArgs& a)
 {
     a.c = c;
     a.chunk = 4096;
-    if (c.v > a.chunk && row_each(c)) {
+    if (row_each(c)) {
         a.chunk = 512;
         a.chunks = (c.v + 511) / 512;                            // at most SEGMENTS
         a.per = 0;
