@@ -420,8 +420,8 @@ def _key(t):
         return None
     try:
         return t.shape, t.stride(), t.dtype, t.get_device()
-    except (AttributeError, TypeError):
-        return (), (), None, -1              # not a tensor: _check says so
+    except (AttributeError, TypeError, RuntimeError):
+        return (), (), None, -1              # not a tensor, or none with strides: _check says so
 
 
 def _check(key, name, dtypes, device=None):

@@ -142,6 +142,28 @@ def test_oracle_segments_are_their_layers(orc):
     assert {(1, False, False), (2, False, False), (1, True, False), (1, False, True), (0, False, False)} <= kinds
 
 
+@pytest.mark.parametrize("dtype", [W.DT_I8, W.DT_BF16], ids=["i8", "bf16"])
+def test_calibration_of_a_network_with_norms(orc, monkeypatch, dtype):
+    """The oracle's calibration goes through the norms, whose scale is the network's own: it stays."""
+    import oracle.calibrate as cal
+    from workloads import nets
+    monkeypatch.setitem(nets.CONFIGS, "norms", (lambda dt: nets._norm_layers(dt, 6, 8, 16, 4, 32), dtype, 0x99))
+    monkeypatch.setitem(cal.SPLITS, "norms", (0.5, 0.5))
+    rec, blob = cal.calibrate("norms", 24)
+    fresh = W.build_net("norms")
+    for op, was, entry in zip(blob.ops, fresh.ops, rec["ops"]):
+        if int(op["kind"]) == W.OP_GROUPNORM:
+            assert entry == dict(shift=int(was["shift"]), res_shift=int(was["res_shift"]))
+        elif int(op["kind"]) == W.OP_CONV and dtype == W.DT_I8:
+            assert entry["shift"] > 0
+    assert np.array_equal(W.apply_calibration(fresh, rec).ops, blob.ops)
+    exited = [e["exited"] for e in rec["exits"]]
+    assert 6 <= exited[0] <= 18 and sum(exited) == 24
+    x = W.input_pool(blob, 24, seed_off=cal.CAL_SEED_OFF)
+    flags = orc.exit_head(blob, 0, orc.stage_forward(blob, 0, x), float(blob.exits[0]["thr"]))[3]
+    assert int(np.count_nonzero(flags)) == exited[0]
+
+
 # ---- on the GPU -------------------------------------------------------------------------------------------------------------------
 @pytest.fixture(scope="module")
 def torch():
@@ -272,4 +294,37 @@ def test_norms_are_timed_in_their_class(torch, ee, orc):
     assert cls["group_norm"]["launches"] == 3 and cls["group_norm"]["ms"] > 0 and cls["group_norm"]["bytes"] > 0
     us = eng.time_layer(1, 4)
     assert (us[0] if isinstance(us, tuple) else us) > 0
+    eng.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [W.DT_I8, W.DT_BF16], ids=["i8", "bf16"])
+def test_segments_captured_in_a_graph(torch, ee, orc, dtype):
+    """Both segments as one graph, norms of one and of two launches among them: every replay, with the program's own work between them, gives the eager results."""
+    blob = W.norm_net(70, 66, 16, 2, dtype, mid=64)
+    eng = ee.Engine(blob, 3)
+    pool = W.input_pool(blob, 12)
+    x = dev(torch, pool[:3])
+    shapes = [blob.stage_out_shape(0), blob.stage_out_shape(1)]
+    want = []
+    for k in range(4):
+        mid = eng.stage_forward(0, dev(torch, pool[3 * k:3 * k + 3]), shapes[0])
+        want.append(eng.stage_forward(1, mid, shapes[1]).clone())
+    torch.cuda.synchronize()
+    eng.close()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        eng = ee.Engine(blob, 3, stream=s)
+        eng.stage_forward(1, eng.stage_forward(0, x, shapes[0]), shapes[1])
+        s.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            out = eng.stage_forward(1, eng.stage_forward(0, x, shapes[0]), shapes[1])
+        for k in (0, 1, 2, 3, 1, 0):
+            x.copy_(dev(torch, pool[3 * k:3 * k + 3]))
+            g.replay()
+            s.synchronize()
+            assert torch.equal(out, want[k]), k
+            torch.ones(1 << 20, device="cuda").sum().item()
+        del g
     eng.close()

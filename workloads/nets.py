@@ -434,6 +434,17 @@ def single_layer_net(kind, h, w, c, k, stride, pad, dtype, seed=0, co=None, act=
 def norm_net(h, w, ci, groups, dtype, seed=0, mid=64):
     """Two segments with group norms where networks have them: behind a convolution, with a ReLU; in front of the residual's sum (the norm adds it); of a concatenation, and writing a slice of one;
     at a segment's border (the first segment ends with one, the second starts with one).  bf16: SiLU in the second.  Data only."""
+    blob = _assemble(_norm_layers(dtype, h, w, ci, groups, mid), dtype, BASE_SEED + 0x7e00 + seed)
+    for op in blob.ops:
+        if int(op["kind"]) == OP_CONV:
+            fan_in = int(op["c_in"]) * int(op["kh"]) * int(op["kw"])
+            op["shift"] = max(0, int(math.ceil(math.log2(2.0 * 74 * 40 * math.sqrt(fan_in) / 127))))
+    for e in blob.exits:
+        e["frac_bits"], e["thr"] = 10, 0.5
+    return blob
+
+
+def _norm_layers(dtype, h, w, ci, groups, mid):
     net = _Net(dtype, h, w, ci, 10)
     t = net.begin_stage()
     t = net.groupnorm(net.conv(t, mid, 3, 1, 1, act="linear"), groups, "relu")
@@ -450,14 +461,7 @@ def norm_net(h, w, ci, groups, dtype, seed=0, mid=64):
     v = net.groupnorm(cat, 4, "none", eps=1e-3, frac_bits=4)
     t = net.groupnorm(net.conv(v, 96, 3, 2, 1, act="linear"), 3, "relu")
     net.end_stage(t)
-    blob = _assemble(net, dtype, BASE_SEED + 0x7e00 + seed)
-    for op in blob.ops:
-        if int(op["kind"]) == OP_CONV:
-            fan_in = int(op["c_in"]) * int(op["kh"]) * int(op["kw"])
-            op["shift"] = max(0, int(math.ceil(math.log2(2.0 * 74 * 40 * math.sqrt(fan_in) / 127))))
-    for e in blob.exits:
-        e["frac_bits"], e["thr"] = 10, 0.5
-    return blob
+    return net
 
 
 def inverted_residual_net(h, w, ci, ce, co, stride, seed=0, blocks=1):
