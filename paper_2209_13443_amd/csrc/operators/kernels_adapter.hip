@@ -182,12 +182,14 @@ __global__ __launch_bounds__(512) void adapter_shrink_kernel(AdapterKernelArgs a
         };
         const int next = NW * a.splits;
         load(std::integral_constant<int, 0>{}, wave + NW * split);
-        for (int c = wave + NW * split; c < chunks; c += 2 * next) {
+        int c = wave + NW * split;
+        for (; c + next < chunks; c += 2 * next) {
             load(std::integral_constant<int, 1>{}, c + next);
             multiply(std::integral_constant<int, 0>{});
             load(std::integral_constant<int, 0>{}, c + 2 * next);
-            multiply(std::integral_constant<int, 1>{});                          // past the end: zeros
+            multiply(std::integral_constant<int, 1>{});
         }
+        if (c < chunks) multiply(std::integral_constant<int, 0>{});              // not past the end: x is zeros there, but the adapter may have infinities
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             if (rank0 + t * ROWS >= a.rp) break;
@@ -284,12 +286,14 @@ __global__ __launch_bounds__(512) void adapter_rows_project_kernel(AdapterKernel
 #pragma unroll
     for (int j = 0; j < J; ++j) load_adapter(j, 0);
     const float bias = a.bias[min(o, a.np - 1)];
-    for (int c = wave; c < chunks; c += 2 * NW) {
+    int c = wave;
+    for (; c + NW < chunks; c += 2 * NW) {
         load(std::integral_constant<int, 1>{}, c + NW);
         multiply(std::integral_constant<int, 0>{});
         load(std::integral_constant<int, 0>{}, c + 2 * NW);
         multiply(std::integral_constant<int, 1>{});
     }
+    if (c < chunks) multiply(std::integral_constant<int, 0>{});                      // not past the end: x is zeros there, but W may have infinities
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -371,36 +375,27 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
         if constexpr (J < XU) dma16(to + (unsigned)(NW * J * 1024), xt + (int64_t)slab(it) * 64, from[J]);
         else dma16(to + (unsigned)(BM * 64 + NW * (J - XU) * 1024), w[J - XU] + (int64_t)slab(it) * 2048, wlane);
     };
-    auto copy = [&](int it) {
-        if ((slab(it) + 1) * 32 <= a.ci) {
-            static_for<XU + WU>([&](auto j) { piece(it, j); });
-            return;
-        }
+    // Piece j of a step that is no whole slab of x for certain.  ad >= 0: slab e of that adapter, where rows of others read zeros; else, e >= 0: past the end, zeros; else a slab of x, with zeros
+    // behind the last column
+    int ids[XU];                                           // the adapters of the rows this lane copies
+    auto piece_of = [&](int it, auto j_tag, int ad, int e) {
+        constexpr int J = decltype(j_tag)::value;
         const unsigned to = lds0 + stage(it) + (unsigned)(wave * 1024);
-#pragma unroll
-        for (int j = 0; j < XU; ++j) {                     // the last columns, where they are no whole 32: zeros behind them
-            const int row = 16 * (j * NW + wave) + (lane >> 2), col = slab(it) * 32 + ((lane & 3) ^ (row >> 2 & 3)) * 8;
-            dma16(to + (unsigned)(NW * j * 1024), col < a.ci ? (const void*)(xt + (int64_t)slab(it) * 64 + from[j]) : a.zeros);
-        }
-        static_for<WU>([&](auto j) { piece(it, std::integral_constant<int, decltype(j)::value + XU>{}); });
-    };
-    // slab e of adapter ad; ad < 0: past the end, zeros
-    auto copy_adapter = [&](int it, int ad, int e) {
-        const unsigned to = lds0 + stage(it) + (unsigned)(wave * 1024);
-#pragma unroll
-        for (int j = 0; j < XU; ++j) {
-            const int row = 16 * (j * NW + wave) + (lane >> 2), k = e * 32 + ((lane & 3) ^ (row >> 2 & 3)) * 8;
-            dma16(to + (unsigned)(NW * j * 1024), ad >= 0 && l_ids[row] == ad && k < kx ? a.u + (int64_t)(m0 + row) * kx + k : a.zeros);
-        }
-#pragma unroll
-        for (int j = 0; j < WU; ++j) {
-            const int u = j * NW + wave;
-            const unsigned char* const b = (const unsigned char*)a.b + (((int64_t)ad * blocks + min(nb0 + u / 2, blocks - 1)) * rs + (e * 2 + u % 2) % rs) * 1024;
-            dma16(to + (unsigned)(BM * 64 + NW * j * 1024), ad >= 0 ? b : (const unsigned char*)a.w, wlane);
+        if constexpr (J < XU) {
+            const int row = 16 * (J * NW + wave) + (lane >> 2), k = ((lane & 3) ^ (row >> 2 & 3)) * 8;
+            const void* at = a.zeros;
+            if (e < 0) at = slab(it) * 32 + k < a.ci ? (const void*)(xt + (int64_t)slab(it) * 64 + from[J]) : at;
+            else if (ad >= 0) at = ids[J] == ad && e * 32 + k < kx ? (const void*)(a.u + (int64_t)(m0 + row) * kx + e * 32 + k) : at;
+            dma16(to + (unsigned)(NW * J * 1024), at);
+        } else {
+            const int u = (J - XU) * NW + wave;
+            const unsigned char* b = w[J - XU] + (int64_t)slab(it) * 2048;
+            if (ad >= 0) b = (const unsigned char*)a.b + (((int64_t)ad * blocks + min(nb0 + u / 2, blocks - 1)) * rs + (e * 2 + u % 2) % rs) * 1024;
+            dma16(to + (unsigned)(BM * 64 + NW * (J - XU) * 1024), e < 0 || ad >= 0 ? (const void*)(b + wlane) : a.zeros);       // zeros past the end: W may have infinities
         }
     };
     constexpr int EARLY = KG <= 2 ? 2 / KG : 0;            // steps that are slabs of x for certain: kp is a multiple of 64
-    static_for<EARLY>([&](auto k) { copy(decltype(k)::value); });
+    static_for<EARLY>([&](auto k) { static_for<XU + WU>([&](auto j) { piece_of(decltype(k)::value, j, -1, -1); }); });
     __syncthreads();
     if (wave_all == 0) {
         int mine[BM / 64], n = 0;
@@ -423,13 +418,16 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
     }
     lds_barrier();
     const int total = slabs + __builtin_amdgcn_readfirstlane(l_list[BM]) * per, iters = (total + KG - 1) / KG;
-    auto copy_any = [&](int it) {
-        const int s = slab(it), e = s - slabs;
-        if (e < 0) copy(it);
-        else copy_adapter(it, s < total ? __builtin_amdgcn_readfirstlane(l_list[e / per]) : -1, s < total ? e % per : 0);
-    };
 #pragma unroll
-    for (int k = EARLY; k < RING - 1; ++k) copy_any(k);
+    for (int j = 0; j < XU; ++j) ids[j] = l_ids[16 * (j * NW + wave) + (lane >> 2)];
+    // f(adapter, its slab) of step `it`, as piece_of takes them
+    auto what = [&](int it, auto&& f) {
+        const int s = slab(it), e = s - slabs;
+        if (e < 0) f(-1, -1);
+        else if (s < total) f(__builtin_amdgcn_readfirstlane(l_list[e / per]), e % per);
+        else f(-1, 0);
+    };
+    for (int k = EARLY; k < RING - 1; ++k) what(k, [&](int ad, int e) { static_for<XU + WU>([&](auto j) { piece_of(k, j, ad, e); }); });
     unsigned at[2];                                        // x, step of 16
 #pragma unroll
     for (int k = 0; k < 2; ++k) at[k] = (unsigned)((wm * MB * 32 + frow) * 64 + (((2 * k + hi) ^ (frow >> 2 & 3)) << 4));
@@ -472,12 +470,17 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
         constexpr int P = decltype(parity)::value;
         constexpr bool FAST = decltype(fast)::value;
         wait_copies_then_barrier<(RING - 3) * (XU + WU)>();      // step it + 1 is there, step it - 1 has been read by all
-        if constexpr (!FAST) copy_any(it + RING - 1);
+        int ad = -1, e = -1;
+        if constexpr (!FAST) what(it + RING - 1, [&](int ad_, int e_) { ad = ad_; e = e_; });
         static_for<2>([&](auto step) {
             constexpr int K = decltype(step)::value;
             multiply(std::integral_constant<int, 2 * P + K>{}, [&](auto k) {
                 spread(k, operands{}, front{}, [&](auto n) { read(std::integral_constant<int, 2 * (1 - P) + K>{}, it + 1, step, n); });
-                if constexpr (FAST && K == 0) spread(k, pieces{}, every{}, [&](auto j) { piece(it + RING - 1, j); });
+                if constexpr (K == 0)
+                    spread(k, pieces{}, every{}, [&](auto j) {
+                        if constexpr (FAST) piece(it + RING - 1, j);
+                        else piece_of(it + RING - 1, j, ad, e);
+                    });
             });
         });
     };

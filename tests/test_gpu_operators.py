@@ -733,3 +733,50 @@ def test_group_norm_int8_values_near_whole_numbers_everywhere(torch, ee):
                 say(f"[case] {pixels} {c} {groups} scale {scale} f {f} rs {rs} residual {r is not None}")
                 ref, _ = norm_ref(torch, x, groups, w, b, 1e-5, "none", r, f, rs)
                 assert torch.equal(ee.group_norm(x, groups, w, b, frac_bits=f, residual=r, res_shift=rs), ref)
+
+
+@pytest.mark.parametrize("rows,ci,co", [(9, 72, 40), (200, 2080, 1000), (512, 1096, 512), (2048, 1096, 1000), (4096, 1096, 1000), (8192, 1096, 1000), (16384, 1064, 1024)])
+def test_adapter_projection_infinite_weights(torch, ee, rows, ci, co):
+    """Infinities in the shared weight, at its first, last and a middle column: the formula's infinities in those outputs, the others as they were.  Reductions of an odd number of slabs."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    say(f"[case] {rows} rows {ci} -> {co}")
+    w = (rnd(co, ci) / ci ** 0.5).bfloat16()
+    a, b = (rnd(16, ci) / ci ** 0.5).bfloat16(), (rnd(co, 16) / 4).bfloat16()
+    odd = w.clone()
+    odd[3, 0], odd[5, ci - 1], odd[co - 1, ci // 2] = float("inf"), -float("inf"), float("inf")
+    x = rnd(rows, ci).bfloat16()
+    ids = torch.randint(-1, 2, (rows,), device="cuda", generator=g, dtype=torch.int32)
+    out = []
+    for weight in (w, odd):
+        proj = ee.AdapterProjection(weight, None, adapters=2, rank=16)
+        proj.load(0, a, b)
+        proj.load(1, b[:ci, :].t().contiguous() if co == ci else a, b, 0.25)
+        out.append(proj(x, ids, dtype=torch.float32))
+    keep = [o for o in range(co) if o not in (3, 5, co - 1)]
+    assert torch.equal(out[0][:, keep], out[1][:, keep]) and out[0].isfinite().all()
+    inf = float("inf")
+    for o, c, sign in ((3, 0, 1.0), (5, ci - 1, -1.0), (co - 1, ci // 2, 1.0)):
+        assert torch.equal(out[1][:, o], sign * inf * torch.sign(x[:, c].float()))
+
+
+@pytest.mark.parametrize("rows,ci,co", [(9, 72, 40), (12, 4096, 64), (300, 520, 200), (1500, 1096, 72)])
+def test_adapter_projection_infinite_first_halves(torch, ee, rows, ci, co):
+    """An infinity in an adapter's first half, at its first, last and a middle column: the formula's infinities in its rows."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    w = (rnd(co, ci) / ci ** 0.5).bfloat16()
+    x = rnd(rows, ci).bfloat16()
+    ids = (torch.arange(rows, device="cuda") % 3).int() - 1
+    b = rnd(co, 2).bfloat16()
+    for col in (0, ci // 2, ci - 1):
+        say(f"[case] {rows} rows {ci} -> {co} column {col}")
+        a = (rnd(2, ci) / ci ** 0.5).bfloat16()
+        a[0, col] = float("inf")
+        proj = ee.AdapterProjection(w, None, adapters=2, rank=16)
+        proj.load(0, a, b)
+        for dtype in (torch.float32, torch.bfloat16):
+            y = proj(x, ids, dtype=dtype)
+            own = ids == 0
+            want = torch.sign(x[own][:, col].float())[:, None] * torch.sign(b[:, 0].float())[None, :] * float("inf")
+            assert torch.equal(y[own].float(), want) and y[~own].isfinite().all()
