@@ -2,7 +2,7 @@
 //
 //   y[m][o] = sum_c x[m][c] W[o][c] + bias[o] + sum_r B_a[o][r] u[m][r],   u[m][r] = scale_a sum_c A_a[r][c] x[m][c],   a: the adapter of row m, or none
 //
-// Two launches.  The first computes u (adapter_shrink_kernel) and the adapter of every row; u is kept as the sum of bf16 numbers (head and remainders:
+// Two launches, or, for long slots and few outputs, one.  The first computes u (adapter_shrink_kernel) and the adapter of every row; u is kept as the sum of bf16 numbers (head and remainders:
 // two of them, relative error 2^-18, for bf16 results, three, 2^-26, for float ones), so that the second half of an adapter runs on the matrix cores as well; few rows keep it in float.  The second is the projection, with the adapters as
 // further steps of its reduction: for each adapter among a tile's rows, the rows of others read zeros.  A second half that has infinities or NaN, which zeros times it would give to the rows of
 // others, is no step: its own rows add it element by element.
@@ -331,11 +331,14 @@ __global__ __launch_bounds__(512) void adapter_rows_project_kernel(AdapterKernel
 // of stages per group filled by asynchronous copies: those of step t + RING - 1 start, and those of t + 1 are waited for, at the barrier in front of step t, so that the operands of a step's
 // first instructions are read before its barrier.
 // The adapters are further slabs: for each different one among the tile's rows, the parts of u (rows of others: zeros) and its second half.
-template <int MB, int NB, int WM, int WN, int KG, int RING, bool F32>
+// FUSE: slots of at least BM - 1 rows, so that a tile has rows of two slots at most, and ranks up to 32: the first halves of both are 64 further outputs of the tile, wavefronts wn = 0 and 1 have one
+// each; they go through LDS to the second halves, and there is no launch in front of this one.
+template <int MB, int NB, int WM, int WN, int KG, int RING, bool F32, bool FUSE>
 __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(AdapterKernelArgs a, int gm, int gn)
 {
-    constexpr int NW = WM * WN, NT = 64 * NW * KG, BM = 32 * MB * WM, BN = 32 * NB * WN, STAGE = (BM + BN) * 64, XU = BM / 16 / NW, WU = BN / 16 / NW;      // XU, WU: KiB a wavefront copies per stage
-    static_assert(XU * 16 * NW == BM && WU * 16 * NW == BN && BM <= 256 && BM % 64 == 0);
+    constexpr int NW = WM * WN, NT = 64 * NW * KG, BM = 32 * MB * WM, BN = 32 * NB * WN, STAGE = (BM + BN + (FUSE ? 64 : 0)) * 64;
+    constexpr int XU = BM / 16 / NW, WU = BN / 16 / NW, AU = FUSE ? 4 / NW : 0, PU = XU + WU + AU;                    // KiB a wavefront copies per stage: of x, of W, of the first halves
+    static_assert(XU * 16 * NW == BM && WU * 16 * NW == BN && BM <= 256 && BM % 64 == 0 && (!FUSE || (WN == 2 && NW == 4 && KG == 1)));
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     int* const l_list = (int*)(lds + KG * RING * STAGE);   // different adapters of the rows, their number
     int* const l_ids = l_list + BM + 4;                    // adapter of every row
@@ -349,7 +352,19 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
     const unsigned lds0 = lds_addr(lds) + (unsigned)(kg * RING * STAGE);
     unsigned char* const ring = lds + kg * RING * STAGE;
     const int slabs = a.kp / 32, blocks = a.np / 32, kx = a.parts * a.rp, per = (kx + 31) / 32, rs = a.rp / 16;      // per: slabs an adapter takes
-    for (int r = tid; r < BM; r += NT) l_ids[r] = m0 + r < a.rows ? a.row_ids ? a.row_ids[m0 + r] : -1 : -2;
+    int two[2] = {-1, -1};                                 // FUSE: the adapters of the tile's slots; l_ids: which of them
+    if constexpr (FUSE) {
+        const int slot = m0 / a.per, last = min(m0 + BM, a.rows) - 1;
+        two[0] = a.ids[slot];
+        two[1] = last / a.per != slot ? a.ids[slot + 1] : -1;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) two[k] = __builtin_amdgcn_readfirstlane((unsigned)two[k] < (unsigned)a.adapters ? two[k] : -1);
+        for (int r = tid; r < BM; r += NT) {
+            const int which = (m0 + r) / a.per != slot;
+            l_ids[r] = m0 + r >= a.rows ? -2 : (which ? two[1] : two[0]) >= 0 ? which : -1;
+        }
+    } else
+        for (int r = tid; r < BM; r += NT) l_ids[r] = m0 + r < a.rows ? a.row_ids ? a.row_ids[m0 + r] : -1 : -2;
     // LDS of a stage: rows of 64 bytes, position p of row r holds chunk p ^ (r / 4 & 3) (16 rows are in 16 different quads of banks) | operands of W, a KiB per block and step of 16
     const unsigned char* const xt = (const unsigned char*)(a.x + (int64_t)m0 * a.ldx);
     unsigned from[XU];                                     // bytes from there: the host bounds 256 rows by 2 GiB
@@ -365,6 +380,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
         w[j] = (const unsigned char*)a.w + ((int64_t)min(nb0 + u / 2, blocks - 1) * slabs * 2 + u % 2) * 1024;
     }
     const unsigned wlane = (unsigned)lane * 16u;
+    const unsigned char* halves = nullptr;                 // FUSE: the first half whose operands this wavefront copies (AU is 1), from its step of 16
+    if constexpr (FUSE) halves = (const unsigned char*)a.a + ((int64_t)max(wave >= 2 ? two[1] : two[0], 0) * slabs * 2 + wave % 2) * 1024;
     // where step `it` goes in the ring, and the slab that is this group's
     auto stage = [&](int it) { return (unsigned)(it % RING * STAGE); };
     auto slab = [&](int it) { return it * KG + kg; };
@@ -373,7 +390,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
         constexpr int J = decltype(j_tag)::value;
         const unsigned to = lds0 + stage(it) + (unsigned)(wave * 1024);
         if constexpr (J < XU) dma16(to + (unsigned)(NW * J * 1024), xt + (int64_t)slab(it) * 64, from[J]);
-        else dma16(to + (unsigned)(BM * 64 + NW * (J - XU) * 1024), w[J - XU] + (int64_t)slab(it) * 2048, wlane);
+        else dma16(to + (unsigned)(BM * 64 + NW * (J - XU) * 1024), (J < XU + WU ? w[J < XU + WU ? J - XU : 0] : halves) + (int64_t)slab(it) * 2048, wlane);
     };
     // Piece j of a step that is no whole slab of x for certain.  ad >= 0: slab e of that adapter, where rows of others read zeros; else, e >= 0: past the end, zeros; else a slab of x, with zeros
     // behind the last column
@@ -389,15 +406,15 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
             dma16(to + (unsigned)(NW * J * 1024), at);
         } else {
             const int u = (J - XU) * NW + wave;
-            const unsigned char* b = w[J - XU] + (int64_t)slab(it) * 2048;
+            const unsigned char* b = (J < XU + WU ? w[J < XU + WU ? J - XU : 0] : halves) + (int64_t)slab(it) * 2048;
             if (ad >= 0) b = (const unsigned char*)a.b + (((int64_t)ad * blocks + min(nb0 + u / 2, blocks - 1)) * rs + (e * 2 + u % 2) % rs) * 1024;
             dma16(to + (unsigned)(BM * 64 + NW * (J - XU) * 1024), e < 0 || ad >= 0 ? (const void*)(b + wlane) : a.zeros);       // zeros past the end: W may have infinities
         }
     };
     constexpr int EARLY = KG <= 2 ? 2 / KG : 0;            // steps that are slabs of x for certain: kp is a multiple of 64
-    static_for<EARLY>([&](auto k) { static_for<XU + WU>([&](auto j) { piece_of(decltype(k)::value, j, -1, -1); }); });
+    static_for<EARLY>([&](auto k) { static_for<PU>([&](auto j) { piece_of(decltype(k)::value, j, -1, -1); }); });
     __syncthreads();
-    if (wave_all == 0) {
+    if (!FUSE && wave_all == 0) {
         int mine[BM / 64], n = 0;
 #pragma unroll
         for (int i = 0; i < BM / 64; ++i) mine[i] = l_ids[64 * i + lane] < ODD ? l_ids[64 * i + lane] : -1;
@@ -417,27 +434,28 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
         if (lane == 0) l_list[BM] = n;
     }
     lds_barrier();
-    const int total = slabs + __builtin_amdgcn_readfirstlane(l_list[BM]) * per, iters = (total + KG - 1) / KG;
+    const int total = FUSE ? slabs : slabs + __builtin_amdgcn_readfirstlane(l_list[BM]) * per, iters = (total + KG - 1) / KG;
 #pragma unroll
     for (int j = 0; j < XU; ++j) ids[j] = l_ids[16 * (j * NW + wave) + (lane >> 2)];
     // f(adapter, its slab) of step `it`, as piece_of takes them
     auto what = [&](int it, auto&& f) {
         const int s = slab(it), e = s - slabs;
         if (e < 0) f(-1, -1);
-        else if (s < total) f(__builtin_amdgcn_readfirstlane(l_list[e / per]), e % per);
+        else if (!FUSE && s < total) f(__builtin_amdgcn_readfirstlane(l_list[e / per]), e % per);
         else f(-1, 0);
     };
-    for (int k = EARLY; k < RING - 1; ++k) what(k, [&](int ad, int e) { static_for<XU + WU>([&](auto j) { piece_of(k, j, ad, e); }); });
+    for (int k = EARLY; k < RING - 1; ++k) what(k, [&](int ad, int e) { static_for<PU>([&](auto j) { piece_of(k, j, ad, e); }); });
     unsigned at[2];                                        // x, step of 16
 #pragma unroll
     for (int k = 0; k < 2; ++k) at[k] = (unsigned)((wm * MB * 32 + frow) * 64 + (((2 * k + hi) ^ (frow >> 2 & 3)) << 4));
     const unsigned wat = (unsigned)(BM * 64 + wn * NB * 2048) + wlane;
     // operands are read two steps of 16 columns before they are used, into four sets in turn: a read takes as long as four to eight matrix instructions when all wavefronts read
-    v4i xv[4][MB], wv[4][NB];
+    v4i xv[4][MB], wv[4][NB], fv[FUSE ? 4 : 1];
     auto read = [&](auto set, int it, auto step, auto n_tag) {           // operand n_tag of a step, in the order they are used: w 0, x 0, the rest of w, the rest of x
         constexpr int S = decltype(set)::value, K = decltype(step)::value, N = decltype(n_tag)::value, X = N == 1 ? 0 : N > NB ? N - NB : -1, W = N == 0 ? 0 : N - 1;
         const unsigned char* const base = ring + stage(it);
-        if constexpr (X >= 0) xv[S][X] = *(const v4i*)(base + at[K] + X * 2048);
+        if constexpr (N == MB + NB) fv[S] = *(const v4i*)(base + (BM + BN) * 64 + wlane + (wn * 2 + K) * 1024);
+        else if constexpr (X >= 0) xv[S][X] = *(const v4i*)(base + at[K] + X * 2048);
         else wv[S][W] = *(const v4i*)(base + wat + (W * 2 + K) * 1024);
     };
     v16f acc[MB][NB];
@@ -445,12 +463,17 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
     for (int i = 0; i < MB; ++i)
 #pragma unroll
         for (int n = 0; n < NB; ++n) acc[i][n] = v16f{};
-    // the MB x NB instructions of a step; behind instruction k: f(k)
+    v16f half[FUSE ? MB : 1];                              // of the first half of adapter two[wn]
+#pragma unroll
+    for (int i = 0; i < (FUSE ? MB : 1); ++i) half[i] = v16f{};
+    // the MB x NB instructions of a step (FUSE: and MB); behind instruction k: f(k)
+    constexpr int INSTRUCTIONS = MB * NB + (FUSE ? MB : 0);
     auto multiply = [&](auto set, auto&& f) {
         constexpr int S = decltype(set)::value;
-        static_for<MB * NB>([&](auto k_tag) {
-            constexpr int K = decltype(k_tag)::value, I = K / NB, N = K % NB;
-            acc[I][N] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, wv[S][N]), __builtin_bit_cast(v8bf, xv[S][I]), acc[I][N], 0, 0, 0);
+        static_for<INSTRUCTIONS>([&](auto k_tag) {
+            constexpr int K = decltype(k_tag)::value, I = K < MB * NB ? K / NB : K - MB * NB, N = K % NB;
+            if constexpr (K >= MB * NB) half[I] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, fv[S]), __builtin_bit_cast(v8bf, xv[S][I]), half[I], 0, 0, 0);
+            else acc[I][N] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, wv[S][N]), __builtin_bit_cast(v8bf, xv[S][I]), acc[I][N], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
             f(k_tag);
             __builtin_amdgcn_sched_barrier(0);
@@ -461,15 +484,15 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
         constexpr int K = decltype(k_tag)::value, COUNT = decltype(count)::value, SLOTS = decltype(slots)::value, LO = K < SLOTS ? K * COUNT / SLOTS : COUNT, HI = K < SLOTS ? (K + 1) * COUNT / SLOTS : COUNT;
         static_for<HI - LO>([&](auto d) { g(std::integral_constant<int, LO + decltype(d)::value>{}); });
     };
-    using operands = std::integral_constant<int, MB + NB>;
-    using pieces = std::integral_constant<int, XU + WU>;
-    using every = std::integral_constant<int, MB * NB>;
-    using front = std::integral_constant<int, (MB * NB + 1) / 2>;
+    using operands = std::integral_constant<int, MB + NB + FUSE>;
+    using pieces = std::integral_constant<int, PU>;
+    using every = std::integral_constant<int, INSTRUCTIONS>;
+    using front = std::integral_constant<int, (INSTRUCTIONS + 1) / 2>;
     // Step `it` of parity P; the copies go out between matrix instructions: all of a workgroup's at once would hold up the instructions behind them
     auto iteration = [&](auto parity, int it, auto fast) {
         constexpr int P = decltype(parity)::value;
         constexpr bool FAST = decltype(fast)::value;
-        wait_copies_then_barrier<(RING - 3) * (XU + WU)>();      // step it + 1 is there, step it - 1 has been read by all
+        wait_copies_then_barrier<(RING - 3) * PU>();      // step it + 1 is there, step it - 1 has been read by all
         int ad = -1, e = -1;
         if constexpr (!FAST) what(it + RING - 1, [&](int ad_, int e_) { ad = ad_; e = e_; });
         static_for<2>([&](auto step) {
@@ -484,8 +507,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
             });
         });
     };
-    wait_copies_then_barrier<(RING - 2) * (XU + WU)>();
-    static_for<2>([&](auto k) { static_for<MB + NB>([&](auto n) { read(k, 0, k, n); }); });
+    wait_copies_then_barrier<(RING - 2) * PU>();
+    static_for<2>([&](auto k) { static_for<MB + NB + FUSE>([&](auto n) { read(k, 0, k, n); }); });
     int it = 0;
     const int full = min(a.ci / 32 / KG, iters) - (RING - 1);   // steps that copy whole slabs of x
     for (; it + 2 <= full; it += 2) static_for<2>([&](auto p) { iteration(p, it + decltype(p)::value, std::true_type{}); });
@@ -494,7 +517,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
 
     // ---- results: a lane has row frow of a block, outputs 8 q + 4 hi + 0..3; through LDS, a wavefront's 32 rows of 32 NB outputs at a time, to whole pieces of 16 bytes ----
     constexpr int ES = F32 ? 4 : 2, VEC = 16 / ES, PIECES = 32 * NB / VEC, PITCH = 32 * NB * ES + 16;
-    constexpr int SUMS = KG > 1 ? (KG - 1) * NW * MB * NB * 4096 : 0;                        // the results' part of LDS is behind the sums'
+    // the results' part of LDS is behind the groups' sums, or the first halves
+    constexpr int PARTS = F32 ? 3 : 2, SUMS = FUSE ? 2 * WM * MB * PARTS * 2048 : KG > 1 ? (KG - 1) * NW * MB * NB * 4096 : 0;
     static_assert(SUMS + NW * 32 * PITCH <= KG * RING * STAGE);
     unsigned char* const mine = lds + SUMS + wave * 32 * PITCH;
     const int first = n0 * 32;
@@ -535,6 +559,73 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void adapter_project_kernel(Adap
                         for (int e = 0; e < 4; ++e) acc[i][n][4 * q + e] += v[e];
                     }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    if constexpr (FUSE) {
+        // first halves as operands in LDS: [adapter][wm][block][part][step of 16][lane][16]; a lane has elements 8 q + 4 hi + 0..3 of its row
+        auto cell = [&](int which, int i, int p, int step) { return lds + ((((which * WM + wm) * MB + i) * PARTS + p) * 2 + step) * 1024; };
+        const int ad = wn ? two[1] : two[0], rank = ad >= 0 ? a.info[ad] >> 1 : 0;
+        const float scale = ad >= 0 ? a.scale[ad] : 0.f;
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = 8 * q + 4 * hi + e < rank ? half[i][4 * q + e] * scale : 0.f;
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    uint16_t h[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const __bf16 b = (__bf16)v[e];
+                        h[e] = __builtin_bit_cast(uint16_t, b);
+                        v[e] = __builtin_isfinite((float)b) ? v[e] - (float)b : 0.f;
+                    }
+                    *(uint2*)(cell(wn, i, p, q >> 1) + (frow + 32 * (q & 1)) * 16 + 8 * hi) = uint2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
+                }
+            }
+        lds_barrier();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (two[k] < 0) continue;
+            const bool odd = a.info[two[k]] & 1;           // infinities: element by element, of the parts' sums
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                if (odd) {
+#pragma unroll
+                    for (int i = 0; i < MB; ++i)
+                        if (l_ids[(wm * MB + i) * 32 + frow] == k)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const int o = min((n0 + n) * 32 + 8 * (e >> 2) + 4 * hi + (e & 3), a.np - 1);
+                                const uint16_t* const b = a.b + ((int64_t)two[k] * blocks + (o >> 5)) * rs * 512 + (o & 31) * 8;
+#pragma unroll 1
+                                for (int r = 0; r < a.rp; ++r) {
+                                    float v = 0.f;
+                                    for (int p = PARTS - 1; p >= 0; --p) v += __uint_as_float((uint32_t)*(const uint16_t*)(cell(k, i, p, r >> 4) + (frow + 32 * (r >> 3 & 1)) * 16 + (r & 7) * 2) << 16);
+                                    acc[i][n][e] = fmaf(v, __uint_as_float((uint32_t)b[(r >> 4) * 512 + (r >> 3 & 1) * 256 + (r & 7)] << 16), acc[i][n][e]);
+                                }
+                            }
+                    continue;
+                }
+                v4i b[2];
+#pragma unroll
+                for (int step = 0; step < 2; ++step) b[step] = *(const v4i*)((const unsigned char*)a.b + (((int64_t)two[k] * blocks + min(n0 + n, blocks - 1)) * rs + min(step, rs - 1)) * 1024 + wlane);
+#pragma unroll
+                for (int i = 0; i < MB; ++i) {
+                    v16f t{};
+#pragma unroll
+                    for (int step = 0; step < 2; ++step)
+                        if (step < rs)
+#pragma unroll
+                            for (int p = 0; p < PARTS; ++p)
+                                t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, b[step]), __builtin_bit_cast(v8bf, *(const v4i*)(cell(k, i, p, step) + wlane)), t, 0, 0, 0);
+                    const bool own = l_ids[(wm * MB + i) * 32 + frow] == k;                  // rows of others keep their sums, whatever the second half holds
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[i][n][e] += own ? t[e] : 0.f;
+                }
+            }
+        }
     }
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
@@ -642,20 +733,30 @@ hipError_t launch_few_rows(const AdapterKernelArgs& k, hipStream_t s)
     return fits(16) ? go(adapter_rows_project_kernel<1>, 1) : fits(32) ? go(adapter_rows_project_kernel<2>, 2) : go(adapter_rows_project_kernel<4>, 4);
 }
 
-template <int MB, int NB, int WM, int WN, int KG, int RING, bool F32>
+template <int MB, int NB, int WM, int WN, int KG, int RING, bool F32, bool FUSE>
 hipError_t launch_tiles(const AdapterKernelArgs& k, hipStream_t s)
 {
     constexpr int BM = 32 * MB * WM, BN = 32 * NB * WN;
-    constexpr unsigned LDS = KG * RING * (BM + BN) * 64 + 8 * BM + 16;
-    static const hipError_t granted = hipFuncSetAttribute(reinterpret_cast<const void*>(&adapter_project_kernel<MB, NB, WM, WN, KG, RING, F32>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    constexpr unsigned LDS = KG * RING * (BM + BN + (FUSE ? 64 : 0)) * 64 + 8 * BM + 16;
+    static const hipError_t granted = hipFuncSetAttribute(reinterpret_cast<const void*>(&adapter_project_kernel<MB, NB, WM, WN, KG, RING, F32, FUSE>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     if (granted != hipSuccess) return granted;
     const int gm = (k.rows + BM - 1) / BM, gn = (k.co + BN - 1) / BN;
-    EE_LAUNCH((adapter_project_kernel<MB, NB, WM, WN, KG, RING, F32>), dim3(xcd_grid((long long)gm * gn)), dim3(64 * WM * WN * KG), LDS, s, k, gm, gn);
+    EE_LAUNCH((adapter_project_kernel<MB, NB, WM, WN, KG, RING, F32, FUSE>), dim3(xcd_grid((long long)gm * gn)), dim3(64 * WM * WN * KG), LDS, s, k, gm, gn);
     return hipGetLastError();
 }
 
-template <int MB, int NB, int WM, int WN, int KG, int RING>
-hipError_t launch_form(const AdapterKernelArgs& k, hipStream_t s) { return k.out_f32 ? launch_tiles<MB, NB, WM, WN, KG, RING, true>(k, s) : launch_tiles<MB, NB, WM, WN, KG, RING, false>(k, s); }
+template <int MB, int NB, int WM, int WN, int KG, int RING, bool FUSE = false>
+hipError_t launch_form(const AdapterKernelArgs& k, hipStream_t s) { return k.out_f32 ? launch_tiles<MB, NB, WM, WN, KG, RING, true, FUSE>(k, s) : launch_tiles<MB, NB, WM, WN, KG, RING, false, FUSE>(k, s); }
+
+// Whether tiles compute the first halves themselves: slots as long as a tile, and outputs that few tiles share, or x would be multiplied with the first halves too often: one column of tiles, or one round
+// of tiles, two columns of them or a short reduction.  Both launches / this, us, rank 32: 12544 rows 1024 -> 128 24.3 / 20.1, -> 256 27.2 / 22.1, -> 512 34 / 38; 38400 rows 4096 -> 128 172 / 122,
+// -> 256 188 / 166, 1024 -> 256 50 / 54; 3136 rows 64 -> 1024 14.7 / 11.4, 512 -> 1024 16.5 / 15.2, 2048 -> 1024 29.9 / 29.9, 1024 -> 128 13.7 / 17.9
+bool fused(const AdapterKernelArgs& k)
+{
+    if (k.offsets || k.adapters == 0 || k.per < 127 || k.rp > 32) return false;
+    const int64_t gn = (k.co + 127) / 128, tiles = (k.rows + 127) / 128 * gn;
+    return gn == 1 ? tiles >= 96 : tiles >= 128 && tiles <= 256 && (gn == 2 || k.kp <= 512);
+}
 
 hipError_t launch_many_rows(const AdapterKernelArgs& k, hipStream_t s)
 {
@@ -723,6 +824,7 @@ hipError_t launch_adapter_project(const AdapterDims& d, const AdapterCall& c, hi
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         k.x = (const uint16_t*)ws; k.ldx = k.kp; k.ci = k.kp;
     }
+    if (k.parts && fused(k)) return launch_form<2, 2, 2, 2, 1, 6, true>(k, s);
     if (d.adapters == 0 && !c.offsets) k.row_ids = nullptr;           // every row has none
     else if (const hipError_t e = launch_shrink(k, s); e != hipSuccess) return e;
     return few_rows(k) ? launch_few_rows(k, s) : launch_many_rows(k, s);

@@ -780,3 +780,43 @@ def test_adapter_projection_infinite_first_halves(torch, ee, rows, ci, co):
             own = ids == 0
             want = torch.sign(x[own][:, col].float())[:, None] * torch.sign(b[:, 0].float())[None, :] * float("inf")
             assert torch.equal(y[own].float(), want) and y[~own].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("slots,per,ci,co,r", [(40, 127, 1096, 250, 32), (33, 128, 520, 256, 16), (9, 333, 2088, 136, 20), (64, 196, 1024, 256, 32), (7, 1001, 264, 72, 1), (30, 150, 1024, 130, 17),
+                                              (3, 5000, 40, 129, 8), (24, 255, 1032, 1000, 32)])
+def test_adapter_projection_long_slots(torch, ee, slots, per, ci, co, r, dtype):
+    """Slots of many rows each, tiles with the end of one and the start of the next, slots without an adapter, adapters of lower rank and with infinities beside sound ones."""
+    g = torch.Generator(device="cuda").manual_seed(slots * per)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    say(f"[case] {slots} x {per} {ci} -> {co} rank {r} {dtype}")
+    w, bias = (rnd(co, ci) / ci ** 0.5).bfloat16(), rnd(co)
+    n = 5
+    proj = ee.AdapterProjection(w, bias, adapters=n, rank=r)
+    ranks = [r, max(1, r // 2), r, 1, r]
+    ab = [((rnd(k, ci) / ci ** 0.5).bfloat16(), (rnd(co, k) / k ** 0.5).bfloat16()) for k in ranks]
+    ab[4][1][co // 2, 0] = float("inf")
+    for i, (a, b) in enumerate(ab):
+        proj.load(i, a, b, 0.5 + i)
+    ids = torch.randint(-1, n, (slots,), device="cuda", generator=g, dtype=torch.int32)
+    ids[0], ids[1] = 4, 2
+    x = rnd(slots, per, ci).bfloat16()
+    out = {"bf16": torch.bfloat16, "fp32": torch.float32}[dtype]
+    y = proj(x, ids, dtype=out)
+    assert torch.equal(y, proj(x, ids, dtype=out)) or ids.eq(4).any()
+    xd, wd = x.double(), w.double().t()
+    ref, size = xd @ wd + bias.double(), xd.abs() @ wd.abs() + bias.double().abs()
+    for s in range(slots):
+        i = int(ids[s])
+        if i >= 0:
+            a, b = ab[i][0].double().t(), ab[i][1].double().t()
+            ref[s] += (0.5 + i) * (xd[s] @ a) @ b
+            size[s] += (0.5 + i) * (xd[s].abs() @ a.abs()) @ b.abs()
+    wild = torch.zeros(slots, 1, co, dtype=torch.bool, device="cuda")
+    wild[ids == 4, :, co // 2] = True
+    wild = wild.expand(slots, per, co)
+    assert torch.equal(y[wild].double(), ref[wild])
+    # the sum of a first half's parts is off by 2^-18 (2^-24) of it
+    part = {"bf16": 2.0 ** -18, "fp32": 2.0 ** -24}[dtype]
+    bad = ((y.double() - ref).abs() > EPS[dtype] * ref.abs() + ((ci + 2 * r + 8) * F32 + part) * size) & ~wild
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}"
