@@ -426,7 +426,8 @@ def _key(t):
 
 def _check(key, name, dtypes, device=None):
     """Of _key(t); returns the device's index (device: the one it has to be)."""
-    _need(key is not None and key[2] in dtypes, f"{name} has to be a tensor of {' or '.join(str(d) for d in dtypes)}", EE_ERR_UNSUPPORTED)
+    if key is None or key[2] not in dtypes:
+        _need(False, f"{name} has to be a tensor of {' or '.join(str(d) for d in dtypes)}", EE_ERR_UNSUPPORTED)
     _need(key[3] >= 0 and (device is None or key[3] == device), "tensors have to be on the GPU, all on the same one")
     return key[3]
 
@@ -527,7 +528,7 @@ class AdapterProjection:
     def __init__(self, weight, bias=None, adapters=0, rank=16):
         at = _check(_key(weight), "weight", (torch.bfloat16,))
         dev = weight.device
-        _need(weight.dim() == 2 and weight.stride(1) == 1, "weight has to be [co, ci] with dense rows")
+        _need(weight.dim() == 2 and (weight.stride(1) == 1 or weight.shape[1] == 1), "weight has to be [co, ci] with dense rows")
         co, ci = weight.shape
         if bias is not None:
             _check(_key(bias), "bias", (torch.float32,), at)
@@ -538,16 +539,18 @@ class AdapterProjection:
         _chk(_lib.ee_adapter_bytes(C.byref(self._dims), C.byref(packed), C.byref(pool)))
         self._packed = torch.empty(packed.value, dtype=torch.uint8, device=dev)
         self._pool = torch.zeros(pool.value, dtype=torch.uint8, device=dev)
-        _on(at, _lib.ee_adapter_pack, C.byref(self._dims), weight.data_ptr(), weight.stride(0), _ptr(bias), self._packed.data_ptr())
+        _on(at, _lib.ee_adapter_pack, C.byref(self._dims), weight.data_ptr(), weight.stride(0) if co > 1 else ci, _ptr(bias), self._packed.data_ptr())
 
     def load(self, i, a, b, scale=1.0):
         """Adapter i becomes scale * b a (a: bfloat16 [r, ci], b: bfloat16 [co, r], r <= rank), for the calls behind this one on its stream."""
-        for t, name in ((a, "a"), (b, "b")):
-            _check(_key(t), name, (torch.bfloat16,), self.device.index)
-            _need(t.dim() == 2 and t.stride(1) == 1 or t.shape[1:] == (1,), f"{name} has to have dense rows")
-        r = a.shape[0]
-        _need(a.shape == (r, self.ci) and b.shape == (self.co, r), "a has to be [r, ci] and b [co, r]")
-        _on(self.device.index, _lib.ee_adapter_load, C.byref(self._dims), i, r, a.data_ptr(), a.stride(0), b.data_ptr(), b.stride(0), scale, self._pool.data_ptr())
+        at, ka, kb = self.device.index, _key(a), _key(b)
+        _check(ka, "a", (torch.bfloat16,), at)
+        _check(kb, "b", (torch.bfloat16,), at)
+        _need(len(ka[0]) == 2 and len(kb[0]) == 2, "a has to be [r, ci] and b [co, r]")
+        r = ka[0][0]
+        _need(ka[0] == (r, self.ci) and kb[0] == (self.co, r), "a has to be [r, ci] and b [co, r]")
+        _need((ka[1][1] == 1 or self.ci == 1) and (kb[1][1] == 1 or r == 1), "a and b have to have dense rows")
+        _on(at, _lib.ee_adapter_load, C.byref(self._dims), i, r, a.data_ptr(), ka[1][0] if r > 1 else self.ci, b.data_ptr(), kb[1][0] if self.co > 1 else r, scale, self._pool.data_ptr())
 
     def unload(self, i):
         _on(self.device.index, _lib.ee_adapter_load, C.byref(self._dims), i, 0, None, 0, None, 0, 0.0, self._pool.data_ptr())

@@ -31,17 +31,21 @@ struct AdapterKernelArgs {
 // ---- layouts -----------------------------------------------------------------------------------------------------------------
 enum { ODD = 1 << 30 };              // in the adapter of a row: its second half has infinities or NaN
 
-// dst[row block][step][lane][8] of src[rows][cols] (zeros outside), blocks x steps of them.  *info becomes 2 rank; where that has been done (mark) its last bit is set if an element is not finite
-__global__ __launch_bounds__(256) void adapter_pack_kernel(const uint16_t* src, int64_t ld, int rows, int cols, uint16_t* dst, int blocks, int steps, int* info, int rank, bool mark)
+// dst[row block][step][lane][8] of src[rows][cols] (zeros outside), blocks x steps of them.  An adapter's first half: *info becomes 2 rank, *scale its factor; its second half behind that (scale null):
+// the last bit of *info is set if an element is not finite
+__global__ __launch_bounds__(256) void adapter_pack_kernel(const uint16_t* src, int64_t ld, int rows, int cols, uint16_t* dst, int blocks, int steps, int* info, int rank, float* scale, float factor)
 {
-    if (info && !mark && blockIdx.x == 0 && threadIdx.x == 0) *info = 2 * rank;
+    if (scale && blockIdx.x == 0 && threadIdx.x == 0) {
+        *info = 2 * rank;
+        *scale = factor;
+    }
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;                 // one 16-byte piece
     if (at >= (int64_t)blocks * steps * 64) return;
     const int lane = (int)(at & 63), row = (int)(at / (64 * (int64_t)steps)) * 32 + (lane & 31), col = (int)(at / 64 % steps) * 16 + (lane >> 5) * 8;
     uint16_t v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = row < rows && col + e < cols ? src[row * ld + col + e] : (uint16_t)0;
-    if (mark) {
+    if (info && !scale) {
         bool odd = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e) odd |= (v[e] & 0x7F80) == 0x7F80;
@@ -57,7 +61,6 @@ __global__ __launch_bounds__(256) void adapter_bias_kernel(const float* src, int
     const int i = blockIdx.x * 256 + threadIdx.x;
     if (i < n_pad) dst[i] = src && i < n ? src[i] : 0.f;
 }
-__global__ void adapter_scale_kernel(float* dst, float v) { *dst = v; }
 
 // rows that are no whole 16-byte pieces: dst[rows][cols_pad] with zeros behind a row's end
 __global__ __launch_bounds__(256) void adapter_rows_kernel(const uint16_t* src, int64_t ld, int rows, int cols, uint16_t* dst, int cols_pad)
@@ -770,9 +773,9 @@ hipError_t launch_many_rows(const AdapterKernelArgs& k, hipStream_t s)
     return (double)((tiles(256, 256) + 255) / 256) < 0.37 * (double)((tiles(128, 128) + 255) / 256) ? launch_form<4, 2, 2, 4, 1, 4>(k, s) : launch_form<2, 2, 2, 2, 1, 4>(k, s);
 }
 
-hipError_t pack(const void* src, int64_t ld, int rows, int cols, void* dst, int64_t blocks, int64_t steps, hipStream_t s, int* info = nullptr, int rank = 0, bool mark = false)
+hipError_t pack(const void* src, int64_t ld, int rows, int cols, void* dst, int64_t blocks, int64_t steps, hipStream_t s, int* info = nullptr, int rank = 0, float* scale = nullptr, float factor = 0.f)
 {
-    EE_LAUNCH(adapter_pack_kernel, dim3((unsigned)((blocks * steps * 64 + 255) / 256)), dim3(256), 0, s, (const uint16_t*)src, ld, rows, cols, (uint16_t*)dst, (int)blocks, (int)steps, info, rank, mark);
+    EE_LAUNCH(adapter_pack_kernel, dim3((unsigned)((blocks * steps * 64 + 255) / 256)), dim3(256), 0, s, (const uint16_t*)src, ld, rows, cols, (uint16_t*)dst, (int)blocks, (int)steps, info, rank, scale, factor);
     return hipGetLastError();
 }
 
@@ -798,12 +801,10 @@ hipError_t launch_adapter_load(const AdapterDims& d, int i, int rank, const void
 {
     const AdapterSizes z(d);
     char* const p = (char*)pool;
-    int* const info = (int*)(p + z.a + z.b) + d.adapters + i;
-    hipError_t e = pack(a, lda, rank, d.ci, p + z.a / d.adapters * i, z.ra / 32, z.kp / 16, s, info, rank);
-    if (e == hipSuccess) e = pack(b, ldb, d.co, rank, p + z.a + z.b / d.adapters * i, z.np / 32, z.rp / 16, s, info, rank, true);
-    if (e != hipSuccess) return e;
-    EE_LAUNCH(adapter_scale_kernel, dim3(1), dim3(1), 0, s, (float*)(p + z.a + z.b) + i, scale);
-    return hipGetLastError();
+    float* const factor = (float*)(p + z.a + z.b) + i;
+    int* const info = (int*)(factor + d.adapters);
+    const hipError_t e = pack(a, lda, rank, d.ci, p + z.a / d.adapters * i, z.ra / 32, z.kp / 16, s, info, rank, factor, scale);
+    return e == hipSuccess ? pack(b, ldb, d.co, rank, p + z.a + z.b / d.adapters * i, z.np / 32, z.rp / 16, s, info, rank) : e;
 }
 
 hipError_t launch_adapter_project(const AdapterDims& d, const AdapterCall& c, hipStream_t s)

@@ -820,3 +820,21 @@ def test_adapter_projection_long_slots(torch, ee, slots, per, ci, co, r, dtype):
     part = {"bf16": 2.0 ** -18, "fp32": 2.0 ** -24}[dtype]
     bad = ((y.double() - ref).abs() > EPS[dtype] * ref.abs() + ((ci + 2 * r + 8) * F32 + part) * size) & ~wild
     assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}"
+
+
+def test_adapter_projection_single_rows_and_columns(torch, ee):
+    """Dimensions of one element have any stride."""
+    g = torch.Generator(device="cuda").manual_seed(12)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g).bfloat16()
+    for ci, co, r in ((24, 40, 1), (1, 5, 1), (9, 1, 3), (1, 1, 1)):
+        say(f"[case] {ci} -> {co} rank {r}")
+        w, a, b, x = rnd(co, ci), rnd(r, ci), rnd(co, r), rnd(3, ci)
+        odd = lambda t: t.as_strided(t.shape, tuple(7 if n == 1 else s for n, s in zip(t.shape, t.stride())))
+        proj = ee.AdapterProjection(odd(w), None, adapters=1, rank=4)
+        proj.load(0, odd(a), odd(b), 2.0)
+        ids = torch.tensor([0, -1, 0], device="cuda", dtype=torch.int32)
+        y = proj(x, ids, dtype=torch.float32).double()
+        ref = x.double() @ w.double().t()
+        ref[[0, 2]] += 2.0 * ((x.double() @ a.double().t()) @ b.double().t())[[0, 2]]
+        size = x.double().abs() @ w.double().t().abs() + 2.0 * (x.double().abs() @ a.double().t().abs()) @ b.double().t().abs()
+        assert bool(((y - ref).abs() <= (ci + r + 8) * F32 * size + 1e-30).all())
