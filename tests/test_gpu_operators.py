@@ -838,3 +838,23 @@ def test_adapter_projection_single_rows_and_columns(torch, ee):
         ref[[0, 2]] += 2.0 * ((x.double() @ a.double().t()) @ b.double().t())[[0, 2]]
         size = x.double().abs() @ w.double().t().abs() + 2.0 * (x.double().abs() @ a.double().t().abs()) @ b.double().t().abs()
         assert bool(((y - ref).abs() <= (ci + r + 8) * F32 * size + 1e-30).all())
+
+
+def test_expanded_pixels(torch, ee):
+    """A dimension repeated by a stride of zero is not one stride apart from the next; all of them repeated are."""
+    x = torch.randn(2, 3, 1, 16, device="cuda").bfloat16()
+    y = torch.randn(2, 3, 1, 5, 16, device="cuda").bfloat16()
+    for bad in (x.expand(2, 3, 4, 16), y.expand(2, 3, 4, 5, 16)):
+        with pytest.raises(ee.EEError) as e:
+            ee.group_norm(bad, 2)
+        assert e.value.code == ee.EE_ERR_ARG
+    proj = ee.AdapterProjection(torch.ones(8, 16, device="cuda").bfloat16())
+    with pytest.raises(ee.EEError):
+        proj(x.expand(2, 3, 4, 16))
+    one = x[:, :1]
+    whole = one.expand(2, 3, 4, 16)
+    assert torch.equal(ee.group_norm(whole, 2), ee.group_norm(whole.contiguous(), 2))
+    res = x.expand(2, 3, 4, 16).contiguous()
+    assert torch.equal(ee.group_norm(res, 2, residual=whole), ee.group_norm(res, 2, residual=whole.contiguous()))
+    samples = x[:1].expand(5, 3, 1, 16)
+    assert torch.equal(ee.group_norm(samples, 2), ee.group_norm(samples.contiguous(), 2))
