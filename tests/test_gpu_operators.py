@@ -858,3 +858,16 @@ def test_expanded_pixels(torch, ee):
     assert torch.equal(ee.group_norm(res, 2, residual=whole), ee.group_norm(res, 2, residual=whole.contiguous()))
     samples = x[:1].expand(5, 3, 1, 16)
     assert torch.equal(ee.group_norm(samples, 2), ee.group_norm(samples.contiguous(), 2))
+
+
+@pytest.mark.parametrize("h,w,c,groups", [(1, 1, 40, 5), (1, 3, 40, 5), (7, 7, 40, 5), (13, 11, 48, 48), (35, 35, 33, 3), (9, 11, 96, 12), (100, 100, 40, 20), (300, 301, 40, 5), (300, 301, 24, 24), (211, 199, 33, 3)])
+def test_group_norm_of_constant_groups_is_the_bias(torch, ee, h, w, c, groups):
+    """Every partial mean of a constant group is the constant and every partial variance 0, whatever the number of values and their size: the result is the bias, not a rounding of it."""
+    bias = torch.linspace(-1, 1, c, device="cuda")
+    say(f"[case] {h}x{w}x{c} groups {groups}")
+    for value in (3.0, -57.25, 1003.0, 65537.0, 1e6, -1.5e10, 1e20, 3e38, 1e-30):
+        x = torch.full((2, h, w, c), value, device="cuda").to(torch.bfloat16)
+        for act in ("none", "relu"):
+            want = (bias if act == "none" else bias.clamp(min=0)).to(torch.bfloat16).expand_as(x)
+            got = ee.group_norm(x, groups, None, bias, act=act)
+            assert torch.equal(got, want), f"{value}: off by {float((got.double() - want.double()).abs().max())}"
