@@ -5,8 +5,8 @@
 //   int8  S1 = sum x, S2 = sum x^2 (exact integers), d = n x - S1, m_c = weight_c 2^f / (n sqrt((n S2 - S1^2) / n^2 + eps)),
 //         y = clamp(floor(d m_c + (bias_c 2^f + 1/2) + res 2^rs), lo, hi) in 64-bit floats: d is exact, so a constant group gives its bias on
 //         every machine and the results are whole numbers that do not depend on the order of a sum; every operation is rounded by itself
-// Statistics of bf16: every lane adds up the differences of its values from one of them, and their squares, has from those its own mean and sum of squared differences from it, and such
-// pairs are merged
+// Statistics of bf16: every lane adds up the differences of at most 64 of its values from one that is near them, and their squares, has from those their mean and sum of squared differences from it, and
+// such pairs are merged
 // (n = na + nb, delta = mb - ma: mean = ma + delta nb / n, M2 = M2a + M2b + delta^2 na nb / n), so that a mean far from zero costs nothing.
 //
 // Bound by memory.  A workgroup has a window of whole groups (columns of 16 bytes, a power of two of them) and some pixels of one sample; a lane has one
@@ -203,20 +203,55 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
     };
 
     if constexpr (FORM != 2) {
-        // bf16: sums of x - pivot and of its square, the pivot a value of the lane's own (its first): as far from the mean as values of the group are.  mean and m2 hold them until all are added.
+        // bf16: sums of x - pivot and of its square, the pivot first a value of the lane's own: as far from the mean as values of the group are.  mean and m2 hold them until 64 values (FORM 0: at most
+        // 32) are added; these become a pair, which is merged with those before (`all`), and the next pivot is the mean up to there, rounded to bf16.  One sum over all values of a lane, up to
+        // 16,384 of them, lost what a first value far from the others left of the variance: 1024 x 1024 pixels of one value but for the first were 10 to 40 % off.
         // Vectors behind the lane's last pixel read as what adds nothing: pivots, int8 zeros
-        stat_t st[GPV] = {};
+        stat_t st[GPV] = {}, all[ES == 2 && FORM == 1 ? GPV : 1] = {};
         float pivot[ES == 2 ? GPV : 1];
         const int values = row < mine ? ((mine - row - 1) >> (LOG_NT - a.wlog)) + 1 : 0;      // vectors of the lane
+        int left = values;                                           // of them not in `all` yet
         raw fill{};
+        auto fill_up = [&] {
+            if constexpr (ES == 2) {
+                if constexpr (VEC == 1) fill = (raw)(__float_as_uint(pivot[0]) >> 16);
+                else
+#pragma unroll
+                    for (int e = 0; e < VEC; e += 2) fill[e >> 1] = (int)(__float_as_uint(pivot[e / SUB]) >> 16 | (__float_as_uint(pivot[(e + 1) / SUB]) & 0xFFFF0000u));
+            }
+        };
         if constexpr (ES == 2) {
 #pragma unroll
             for (int j = 0; j < GPV; ++j) pivot[j] = values ? P::f(data[0], j * SUB) : 0.f;
-            if constexpr (VEC == 1) fill = values ? data[0] : raw{};
-            else
-#pragma unroll
-                for (int e = 0; e < VEC; e += 2) fill[e >> 1] = (int)(__float_as_uint(pivot[e / SUB]) >> 16 | (__float_as_uint(pivot[(e + 1) / SUB]) & 0xFFFF0000u));
+            fill_up();
         }
+        // the sums of `vectors` vectors become the number of values, their mean and the sum of squared differences from it
+        auto pairs = [&](int vectors) {
+            if constexpr (ES == 2) {
+                const float n = (float)(vectors * SUB), inv = __builtin_amdgcn_rcpf(fmaxf(n, 1.f));
+#pragma unroll
+                for (int j = 0; j < GPV; ++j) {
+                    const float d = st[j].mean * inv;
+                    st[j].n = n;
+                    st[j].m2 = fmaxf(fmaf(-d, st[j].mean, st[j].m2), 0.f) + 0.f * st[j].m2;      // not below 0 by rounding; a NaN stays one
+                    st[j].mean = pivot[j] + d;
+                }
+            }
+        };
+        auto merge_all = [&](int vectors) {
+            if constexpr (ES == 2 && FORM == 1) {
+                vectors = min(vectors, left);
+                left -= vectors;
+                pairs(vectors);
+#pragma unroll
+                for (int j = 0; j < GPV; ++j) {
+                    merge(all[j], st[j].n, st[j].mean, st[j].m2);
+                    st[j] = stat_t{};
+                    pivot[j] = (float)(__bf16)all[j].mean;
+                }
+                fill_up();
+            }
+        };
         auto add = [&](raw (&v)[NV], int base) {
             if (base + NV * rows > count)
 #pragma unroll
@@ -257,7 +292,9 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
         };
         if constexpr (FORM == 0) add(data, 0);
         else {                                                       // the next pixels are on their way while these are added
+            constexpr int TURNS = std::max(1, 64 / (2 * NV * SUB));  // that add 64 values
             raw d2[NV];
+            int turn = 0;
 #pragma unroll 1
             for (int base = 0; base < count; base += 2 * NV * rows) {
 #pragma unroll
@@ -266,18 +303,17 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
 #pragma unroll
                 for (int i = 0; i < NV; ++i) data[i] = x.load(base + (2 * NV + i) * rows);
                 add(d2, base + NV * rows);
+                if (ES == 2 && ++turn == TURNS) {
+                    turn = 0;
+                    merge_all(TURNS * 2 * NV);
+                }
             }
         }
-        if constexpr (ES == 2) {
-            const float n = (float)values * SUB, inv = __builtin_amdgcn_rcpf(fmaxf(n, 1.f));
+        if constexpr (ES == 2 && FORM == 1) {
+            merge_all(left);
 #pragma unroll
-            for (int j = 0; j < GPV; ++j) {
-                const float d = st[j].mean * inv;
-                st[j].n = n;
-                st[j].m2 = fmaxf(fmaf(-d, st[j].mean, st[j].m2), 0.f) + 0.f * st[j].m2;      // not below 0 by rounding; a NaN stays one
-                st[j].mean = pivot[j] + d;
-            }
-        }
+            for (int j = 0; j < GPV; ++j) st[j] = all[j];
+        } else pairs(values);
         // lanes of a wavefront with the same column, then slices of the workgroup through LDS
 #pragma unroll 1
         for (int off = cols; off < 64; off <<= 1) {

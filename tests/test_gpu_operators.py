@@ -871,3 +871,37 @@ def test_group_norm_of_constant_groups_is_the_bias(torch, ee, h, w, c, groups):
             want = (bias if act == "none" else bias.clamp(min=0)).to(torch.bfloat16).expand_as(x)
             got = ee.group_norm(x, groups, None, bias, act=act)
             assert torch.equal(got, want), f"{value}: off by {float((got.double() - want.double()).abs().max())}"
+
+
+@pytest.mark.parametrize("h,w,c", [(64, 64, 64), (300, 301, 40), (512, 512, 256), (512, 512, 512), (1024, 1024, 256), (2048, 2048, 64), (700, 701, 33)])
+@pytest.mark.parametrize("cpg", [8, 2, 1])
+def test_group_norm_of_a_constant_and_one_pixel_apart(torch, ee, h, w, c, cpg):
+    """One pixel is 0, all others one value v: the variance is that pixel's alone, v^2 (n - 1) / n^2 with n pixels, wherever it lies.  Bound of the result: half a step of bf16, and half of what the
+    variance may be off by: 64 values are added from a pivot that is v off at most, 63 additions of up to 64 v^2 each within 2^-24, 2^-12 of v^2; twice that for the mean's part and the merges."""
+    groups = c // cpg if c % cpg == 0 else c // 3
+    n = h * w
+    say(f"[case] {h}x{w}x{c} groups {groups}")
+    for value in (57.25, 100.5, 3.3125):
+        for at in (0, 1, n // 2, n - 1):
+            x = torch.full((1, n, c), value, device="cuda", dtype=torch.bfloat16)
+            x[0, at] = 0
+            y = ee.group_norm(x.view(1, h, w, c), groups, eps=0.0).view(n, c)
+            a = n / (value * (n - 1) ** 0.5)
+            apart, others = (1 / n - 1) * value * a, value / n * a
+            mean = 128 * F32 * 2 * value * a
+            assert float((y[at].double() - apart).abs().max()) <= (2.0 ** -8 + 2.0 ** -11) * abs(apart) + mean, (value, at, float(y[at, 0]), apart)
+            y[at] = others
+            assert float((y.float() - others).abs().max()) <= (2.0 ** -8 + 2.0 ** -11) * others + mean, (value, at)
+
+
+def test_group_norm_of_large_maps_against_64_bits(torch, ee):
+    """Long lanes over values that drift from the first pixel to the last and are far from zero: every part's mean is another one."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for h, w, c, groups, level, drift in ((512, 512, 256, 32, 0.0, 0.0), (700, 511, 64, 32, 200.0, 50.0), (1024, 1024, 64, 8, -1000.0, 300.0), (513, 512, 33, 3, 5.0, 40.0)):
+        say(f"[case] {h}x{w}x{c} groups {groups} level {level} drift {drift}")
+        x = (torch.randn(1, h * w, c, device="cuda", generator=g) * 4 + level + drift * torch.linspace(0, 1, h * w, device="cuda").view(1, -1, 1)).bfloat16()
+        x[0, 0] = 0
+        ref, tol = norm_ref(torch, x, groups, None, None, 1e-5, "none", None)
+        got = ee.group_norm(x.view(1, h, w, c), groups).view(x.shape)
+        off = (got.double() - ref).abs() - tol
+        assert float(off.max()) <= 0, f"off by {float(off.max())} more than the bound"
