@@ -221,7 +221,7 @@ hipError_t ee_ctx::timed(int cls, double ops, double bytes, F&& launch, int op)
     }
     ee::ProfRec& r = prof[prof_used++];
     r.cls = cls; r.op = op; r.ops = ops; r.bytes = bytes;
-    ee::g_launch_start = r.e0;                    // attached to the dispatch (of the last kernel, if `launch` issues several)
+    ee::g_launch_start = r.e0;                    // attached to the dispatch; where `launch` issues several kernels it says which has which
     ee::g_launch_stop = r.e1;
     hipError_t e = launch();
     ee::g_launch_start = ee::g_launch_stop = nullptr;

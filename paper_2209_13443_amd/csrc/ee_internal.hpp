@@ -147,6 +147,18 @@ struct PoolArgs {         // depthwise 3x3 and max-pool share the shape block
 // to the dispatch itself (its own begin and end time stamps, what a kernel trace shows), instead of event records in
 // front of and behind it, which would also count the dispatch latency of a stream whose back-to-back launches they break.
 extern thread_local hipEvent_t g_launch_start, g_launch_stop;     // null: an ordinary launch
+// Several kernels timed as one: the pair's first event goes with the first of them, its second with the last.  before(): in front of each, `last` in front of the last one
+struct TimedLaunches {
+    const hipEvent_t start = g_launch_start, stop = g_launch_stop;
+    bool first = true;
+    void before(bool last)
+    {
+        g_launch_start = first ? start : nullptr;
+        g_launch_stop = last ? stop : nullptr;
+        first = false;
+    }
+    ~TimedLaunches() { g_launch_start = start; g_launch_stop = stop; }
+};
 #define EE_LAUNCH(kernel, grid, block, lds_bytes, stream, ...) \
     hipExtLaunchKernelGGL(kernel, grid, block, lds_bytes, stream, ee::g_launch_start, ee::g_launch_stop, 0, __VA_ARGS__)
 

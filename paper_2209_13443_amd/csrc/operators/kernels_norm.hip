@@ -627,15 +627,18 @@ hipError_t launch_norm_form(const NormKernelArgs& k, hipStream_t s)
 }
 
 template <int ES, int VEC, int GPV>
-hipError_t launch_norm_gpv(const NormKernelArgs& k, const NormPlan& p, hipStream_t s)
+hipError_t launch_norm_gpv(const NormKernelArgs& k, const NormPlan& p, hipStream_t s, TimedLaunches& timed, bool last)
 {
+    timed.before(last && !p.split);
     if (p.split && p.nt == 256) {
         const hipError_t e = launch_norm_form<ES, VEC, GPV, 256, 4, 1>(k, s);
         if (e != hipSuccess) return e;
+        timed.before(last);
         return p.past ? launch_norm_form<ES, VEC, GPV, 256, 4, 2, true>(k, s) : launch_norm_form<ES, VEC, GPV, 256, 4, 2>(k, s);
     }
     if (p.split) {
         const hipError_t e = launch_norm_form<ES, VEC, GPV, 1024, 4, 1>(k, s);
+        timed.before(last);
         return e == hipSuccess ? launch_norm_form<ES, VEC, GPV, 1024, 4, 2>(k, s) : e;
     }
     if (p.nt == 256) return p.nv == 1 ? launch_norm_form<ES, VEC, GPV, 256, 1, 0>(k, s) : launch_norm_form<ES, VEC, GPV, 256, 4, 0>(k, s);
@@ -684,11 +687,13 @@ hipError_t launch_group_norm(const NormArgs& a, void* workspace, hipStream_t s)
     k.hi = a.act == EE_ACT_RELU6 ? (int)std::min(127.0, 6.0 * k.out_scale) : 127;
     const int64_t es = a.dtype == EE_I8 ? 1 : 2;
     auto at = [&](const void* base, int b, int64_t sample) { return base ? (void*)((char*)base + b * sample * es) : nullptr; };
+    TimedLaunches timed;
     for (int b = 0; b < a.b; b += p.batch) {
+        const bool last = a.b - b <= p.batch;
         k.x = at(a.x, b, a.x_sample); k.res = at(a.res, b, a.res_sample); k.y = at(a.y, b, a.y_sample);
         k.units = std::min(p.batch, a.b - b) * p.chunks * p.windows;
-        const hipError_t e = a.dtype == EE_I8 ? (p.vec == 1 ? launch_norm_gpv<1, 1, 1>(k, p, s) : p.gpv == 1 ? launch_norm_gpv<1, 16, 1>(k, p, s) : p.gpv == 4 ? launch_norm_gpv<1, 16, 4>(k, p, s) : launch_norm_gpv<1, 16, 16>(k, p, s))
-                           : p.vec == 1 ? launch_norm_gpv<2, 1, 1>(k, p, s) : p.gpv == 1 ? launch_norm_gpv<2, 8, 1>(k, p, s) : p.gpv == 4 ? launch_norm_gpv<2, 8, 4>(k, p, s) : launch_norm_gpv<2, 8, 8>(k, p, s);
+        const hipError_t e = a.dtype == EE_I8 ? (p.vec == 1 ? launch_norm_gpv<1, 1, 1>(k, p, s, timed, last) : p.gpv == 1 ? launch_norm_gpv<1, 16, 1>(k, p, s, timed, last) : p.gpv == 4 ? launch_norm_gpv<1, 16, 4>(k, p, s, timed, last) : launch_norm_gpv<1, 16, 16>(k, p, s, timed, last))
+                           : p.vec == 1 ? launch_norm_gpv<2, 1, 1>(k, p, s, timed, last) : p.gpv == 1 ? launch_norm_gpv<2, 8, 1>(k, p, s, timed, last) : p.gpv == 4 ? launch_norm_gpv<2, 8, 4>(k, p, s, timed, last) : launch_norm_gpv<2, 8, 8>(k, p, s, timed, last);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

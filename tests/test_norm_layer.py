@@ -328,3 +328,36 @@ def test_segments_captured_in_a_graph(torch, ee, orc, dtype):
             torch.ones(1 << 20, device="cuda").sum().item()
         del g
     eng.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("h,c,b", [(10, 64, 4), (96, 64, 40), (112, 64, 256)])
+def test_timed_norms_cover_all_their_launches(torch, ee, orc, h, c, b):
+    """A layer of one launch, of two, and of two for each of two parts of the batch: the profile's time is from the first one's begin to the last one's end, so no less than seven tenths of what the layer
+    takes among others like it, where the last launch alone is at most six tenths of two and a third of four."""
+    blob = W.norm_net(10, 12, 16, 8, W.DT_BF16)
+    keep = W.Blob(blob.tobytes())
+    keep.ops[0] = next(o for o in blob.ops if int(o["kind"]) == W.OP_GROUPNORM)
+    for k, v in (("src", 0), ("dst", 1), ("res", -1), ("h_in", h), ("w_in", h), ("c_in", c), ("h_out", h), ("w_out", h), ("c_out", c), ("c_off", 0), ("c_tot", c), ("aux", 8)):
+        keep.ops[0][k] = v
+    keep.header[0]["n_stages"] = 1
+    for k, v in (("in_h", h), ("in_w", h), ("in_c", c)):
+        keep.header[0][k] = v
+    for k, v in (("n_ops", 1), ("n_tensors", 2), ("out_tensor", 1), ("out_h", h), ("out_w", h), ("out_c", c)):
+        keep.stages[0][k] = v
+    for k, v in (("h", h), ("w", h), ("c", c)):
+        keep.exits[0][k] = v
+    assert orc.blob_check(keep) == 0
+    eng = ee.Engine(keep, b)
+    x = torch.randn(b, h, h, c, device="cuda").bfloat16().view(torch.int16)
+    eng.stage_forward(0, x, (h, h, c))
+    alone = eng.time_layer(0, b)[0]
+    eng.profile(1)
+    reps = 20
+    for _ in range(reps):
+        eng.stage_forward(0, x, (h, h, c))
+    cls, layers = eng.profile_read(len(keep.ops))
+    say(f"[case] {b} x {h}x{h}x{c}: {alone:.1f} us a layer, profile {1e3 * layers[0]['ms'] / reps:.1f}")
+    assert cls["group_norm"]["launches"] == layers[0]["launches"] == reps
+    assert 1e3 * layers[0]["ms"] / reps >= (0.7 if h > 10 else 0.2) * alone
+    eng.close()
