@@ -612,6 +612,8 @@ NormPlan plan_norm(const NormArgs& a, bool aligned)
     const int full = a.dtype == EE_I8 ? 16 : 8;
     p.ok = (aligned && a.c % full == 0 && plan_norm_vec(part, full, p)) || plan_norm_vec(part, 1, p);
     p.batch = p.split ? part.b : a.b;
+    // a launch has less than 2^32 threads, and xcd_unit counts up to 2^28 workgroups: more samples than that are worked through in parts
+    if (p.ok) p.batch = (int)std::min<int64_t>(p.batch, std::min((1ll << 32) / p.nt - 8, (1ll << 28) - 8) / ((int64_t)p.chunks * p.windows));
     // a large result is written past the caches: left in them, writing it back would fall on the next kernel.  64 x 56x56x256 bf16 with residual, both launches 89 -> 77 us, 256 x 112x112x64 247 -> 232
     p.past = (double)a.b * a.pixels * a.c * (a.dtype == EE_I8 ? 1 : 2) >= 64e6;
     return p;
@@ -656,11 +658,8 @@ bool norm_aligned(const NormArgs& a)
 
 bool group_norm_supported(const NormArgs& a) { return plan_norm(a, norm_aligned(a)).ok; }
 
-bool group_norm_grid_fits(const NormArgs& a)
-{
-    const NormPlan p = plan_norm(a, norm_aligned(a));
-    return (int64_t)p.batch * p.chunks * p.windows < 1ll << 28;
-}
+// one sample does
+bool group_norm_grid_fits(const NormArgs& a) { return a.b == 0 || plan_norm(a, norm_aligned(a)).batch > 0; }
 
 // a call whose alignment is not known yet may be cut either way
 size_t group_norm_workspace(const NormArgs& a)
@@ -686,12 +685,12 @@ hipError_t launch_group_norm(const NormArgs& a, void* workspace, hipStream_t s)
     k.lo = a.act == EE_ACT_NONE ? -128 : 0;
     k.hi = a.act == EE_ACT_RELU6 ? (int)std::min(127.0, 6.0 * k.out_scale) : 127;
     const int64_t es = a.dtype == EE_I8 ? 1 : 2;
-    auto at = [&](const void* base, int b, int64_t sample) { return base ? (void*)((char*)base + b * sample * es) : nullptr; };
+    auto at = [&](const void* base, int64_t b, int64_t sample) { return base ? (void*)((char*)base + b * sample * es) : nullptr; };
     TimedLaunches timed;
-    for (int b = 0; b < a.b; b += p.batch) {
+    for (int64_t b = 0; b < a.b; b += p.batch) {
         const bool last = a.b - b <= p.batch;
         k.x = at(a.x, b, a.x_sample); k.res = at(a.res, b, a.res_sample); k.y = at(a.y, b, a.y_sample);
-        k.units = std::min(p.batch, a.b - b) * p.chunks * p.windows;
+        k.units = (int)std::min<int64_t>(p.batch, a.b - b) * p.chunks * p.windows;
         const hipError_t e = a.dtype == EE_I8 ? (p.vec == 1 ? launch_norm_gpv<1, 1, 1>(k, p, s, timed, last) : p.gpv == 1 ? launch_norm_gpv<1, 16, 1>(k, p, s, timed, last) : p.gpv == 4 ? launch_norm_gpv<1, 16, 4>(k, p, s, timed, last) : launch_norm_gpv<1, 16, 16>(k, p, s, timed, last))
                            : p.vec == 1 ? launch_norm_gpv<2, 1, 1>(k, p, s, timed, last) : p.gpv == 1 ? launch_norm_gpv<2, 8, 1>(k, p, s, timed, last) : p.gpv == 4 ? launch_norm_gpv<2, 8, 4>(k, p, s, timed, last) : launch_norm_gpv<2, 8, 8>(k, p, s, timed, last);
         if (e != hipSuccess) return e;

@@ -905,3 +905,18 @@ def test_group_norm_of_large_maps_against_64_bits(torch, ee):
         got = ee.group_norm(x.view(1, h, w, c), groups).view(x.shape)
         off = (got.double() - ref).abs() - tol
         assert float(off.max()) <= 0, f"off by {float(off.max())} more than the bound"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "int8"])
+def test_group_norm_more_samples_than_a_launch_has_workgroups(torch, ee, dtype):
+    """2^24 workgroups of 256 threads are as many threads as a launch may not have."""
+    b, c, groups = (1 << 24) + 5, 16, 4
+    g = torch.Generator(device="cuda").manual_seed(24)
+    x = torch.randint(-100, 100, (b, c), device="cuda", generator=g, dtype=torch.int8)
+    x = x if dtype == "int8" else x.bfloat16()
+    say(f"[case] {b} samples {dtype}")
+    got = ee.group_norm(x, groups, frac_bits=4)
+    for first in list(range(0, b, 1 << 21)) + [b - 9]:
+        part = slice(first, first + (1 << 21))
+        ref, bound = norm_ref(torch, x[part, None], groups, None, None, 1e-5, "none", None, 4)
+        assert torch.equal(got[part, None], ref) if bound is None else bool(((got[part, None].double() - ref).abs() <= bound).all()), first
