@@ -31,6 +31,9 @@ struct AdapterKernelArgs {
 // ---- layouts -----------------------------------------------------------------------------------------------------------------
 enum { ODD = 1 << 30 };              // in the adapter of a row: its second half has infinities or NaN
 
+// A launch has less than 2^32 threads, and layouts may have more elements: these kernels' threads take every so many'th of them
+unsigned blocks_of(int64_t threads) { return (unsigned)std::min<int64_t>((threads + 255) / 256, 1 << 23); }
+
 // dst[row block][step][lane][8] of src[rows][cols] (zeros outside), blocks x steps of them.  An adapter's first half: *info becomes 2 rank, *scale its factor; its second half behind that (scale null):
 // the last bit of *info is set if an element is not finite
 __global__ __launch_bounds__(256) void adapter_pack_kernel(const uint16_t* src, int64_t ld, int rows, int cols, uint16_t* dst, int blocks, int steps, int* info, int rank, float* scale, float factor)
@@ -39,21 +42,21 @@ __global__ __launch_bounds__(256) void adapter_pack_kernel(const uint16_t* src, 
         *info = 2 * rank;
         *scale = factor;
     }
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;                 // one 16-byte piece
-    if (at >= (int64_t)blocks * steps * 64) return;
-    const int lane = (int)(at & 63), row = (int)(at / (64 * (int64_t)steps)) * 32 + (lane & 31), col = (int)(at / 64 % steps) * 16 + (lane >> 5) * 8;
-    uint16_t v[8];
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < (int64_t)blocks * steps * 64; at += (int64_t)gridDim.x * 256) {      // 16-byte pieces
+        const int lane = (int)(at & 63), row = (int)(at / (64 * (int64_t)steps)) * 32 + (lane & 31), col = (int)(at / 64 % steps) * 16 + (lane >> 5) * 8;
+        uint16_t v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = row < rows && col + e < cols ? src[row * ld + col + e] : (uint16_t)0;
-    if (info && !scale) {
-        bool odd = false;
+        for (int e = 0; e < 8; ++e) v[e] = row < rows && col + e < cols ? src[row * ld + col + e] : (uint16_t)0;
+        if (info && !scale) {
+            bool odd = false;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) odd |= (v[e] & 0x7F80) == 0x7F80;
-        if (odd) *info = 2 * rank + 1;                     // by all that find one
+            for (int e = 0; e < 8; ++e) odd |= (v[e] & 0x7F80) == 0x7F80;
+            if (odd) *info = 2 * rank + 1;                 // by all that find one
+        }
+        v4i o;
+        __builtin_memcpy(&o, v, 16);
+        *(v4i*)(dst + at * 8) = o;
     }
-    v4i o;
-    __builtin_memcpy(&o, v, 16);
-    *(v4i*)(dst + at * 8) = o;
 }
 
 __global__ __launch_bounds__(256) void adapter_bias_kernel(const float* src, int n, float* dst, int n_pad)
@@ -65,11 +68,11 @@ __global__ __launch_bounds__(256) void adapter_bias_kernel(const float* src, int
 // rows that are no whole 16-byte pieces: dst[rows][cols_pad] with zeros behind a row's end
 __global__ __launch_bounds__(256) void adapter_rows_kernel(const uint16_t* src, int64_t ld, int rows, int cols, uint16_t* dst, int cols_pad)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= (int64_t)rows * cols_pad) return;
-    const int64_t row = at / cols_pad;
-    const int col = (int)(at - row * cols_pad);
-    dst[at] = col < cols ? src[row * ld + col] : (uint16_t)0;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < (int64_t)rows * cols_pad; at += (int64_t)gridDim.x * 256) {
+        const int64_t row = at / cols_pad;
+        const int col = (int)(at - row * cols_pad);
+        dst[at] = col < cols ? src[row * ld + col] : (uint16_t)0;
+    }
 }
 
 // ---- first halves ------------------------------------------------------------------------------------------------------------
@@ -775,7 +778,7 @@ hipError_t launch_many_rows(const AdapterKernelArgs& k, hipStream_t s)
 
 hipError_t pack(const void* src, int64_t ld, int rows, int cols, void* dst, int64_t blocks, int64_t steps, hipStream_t s, int* info = nullptr, int rank = 0, float* scale = nullptr, float factor = 0.f)
 {
-    EE_LAUNCH(adapter_pack_kernel, dim3((unsigned)((blocks * steps * 64 + 255) / 256)), dim3(256), 0, s, (const uint16_t*)src, ld, rows, cols, (uint16_t*)dst, (int)blocks, (int)steps, info, rank, scale, factor);
+    EE_LAUNCH(adapter_pack_kernel, dim3(blocks_of(blocks * steps * 64)), dim3(256), 0, s, (const uint16_t*)src, ld, rows, cols, (uint16_t*)dst, (int)blocks, (int)steps, info, rank, scale, factor);
     return hipGetLastError();
 }
 
@@ -821,7 +824,7 @@ hipError_t launch_adapter_project(const AdapterDims& d, const AdapterCall& c, hi
     k.u = (uint16_t*)ws; ws += up(u_bytes(c.rows) * c.rows * z.rp, 256);
     k.row_ids = (int*)ws; ws += up(4ll * c.rows, 256);
     if (((uintptr_t)c.x & 15) || c.ldx % 8 || d.ci % 8 || c.ldx > 1 << 21) {
-        EE_LAUNCH(adapter_rows_kernel, dim3((unsigned)(((int64_t)c.rows * z.kp + 255) / 256)), dim3(256), 0, s, k.x, k.ldx, c.rows, d.ci, (uint16_t*)ws, k.kp);
+        EE_LAUNCH(adapter_rows_kernel, dim3(blocks_of((int64_t)c.rows * z.kp)), dim3(256), 0, s, k.x, k.ldx, c.rows, d.ci, (uint16_t*)ws, k.kp);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         k.x = (const uint16_t*)ws; k.ldx = k.kp; k.ci = k.kp;
     }

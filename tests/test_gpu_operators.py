@@ -920,3 +920,23 @@ def test_group_norm_more_samples_than_a_launch_has_workgroups(torch, ee, dtype):
         part = slice(first, first + (1 << 21))
         ref, bound = norm_ref(torch, x[part, None], groups, None, None, 1e-5, "none", None, 4)
         assert torch.equal(got[part, None], ref) if bound is None else bool(((got[part, None].double() - ref).abs() <= bound).all()), first
+
+
+def test_adapter_projection_copies_more_elements_than_a_launch_has_threads(torch, ee):
+    """Rows that are no whole 16-byte pieces, more than 2^32 elements with their padding: all of them are copied and projected."""
+    rows, ci, co = (1 << 21) + 77, 2047, 8
+    g = torch.Generator(device="cuda").manual_seed(32)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    x = torch.empty(rows, ci, device="cuda", dtype=torch.bfloat16)
+    for first in range(0, rows, 1 << 18):
+        x[first:first + (1 << 18)] = rnd(min(1 << 18, rows - first), ci)
+    w, ad = (rnd(co, ci) / ci ** 0.5).bfloat16(), adapters_of(torch, g, 1, 4, ci, co)
+    proj = ee.AdapterProjection(w, None, adapters=1, rank=4)
+    proj.load(0, *ad[0])
+    ids = (torch.arange(rows, device="cuda", dtype=torch.int32) % 2) - 1
+    say(f"[case] {rows} x {ci} -> {co}")
+    got = proj(x, ids, dtype=torch.float32)
+    for first in (0, (1 << 20) - 9, rows - (1 << 14)):
+        part = slice(first, first + (1 << 14))
+        ref, tol = project_ref(torch, x[part], w, None, ad, ids[part], "fp32")
+        assert bool(((got[part].double() - ref).abs() <= tol).all()), first
