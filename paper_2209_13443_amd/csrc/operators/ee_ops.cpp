@@ -23,7 +23,7 @@ int check_norm(const ee_norm_desc* d, NormArgs& a)
             if (stride < 0) return EE_ERR_ARG;
         if (d->y_pixel < d->c) return EE_ERR_ARG;
         for (const int64_t stride : {d->x_pixel, d->res_pixel, d->y_pixel})
-            if (stride >= 1 << 20 || ((d->pixels + 1024) * stride + d->c) * es >= 1ll << 31) return EE_ERR_OVERFLOW;
+            if (stride >= 1 << 20 || ((d->pixels + 1024ll) * stride + d->c) * es >= 1ll << 31) return EE_ERR_OVERFLOW;
     }
     a = NormArgs{};
     a.dtype = d->dtype; a.act = d->act; a.b = d->b; a.pixels = d->pixels; a.c = d->c; a.groups = d->groups; a.frac_bits = d->frac_bits; a.res_shift = d->res_shift; a.eps = d->eps;

@@ -121,3 +121,12 @@ def test_group_norm_refuses_layouts(ee):
     for k in [dict(y_sample=-49 * 64), dict(y_sample=64, y_pixel=128), dict(b=1, y_sample=0), dict(pixels=1, y_sample=64, y_pixel=0, x_pixel=-5), dict(x_sample=0), dict(x_pixel=0, res_pixel=0),
               dict(b=0, y_sample=0), dict(pixels=0, y_sample=0)]:
         both(ee.EE_OK, **k)
+
+
+def test_group_norm_refuses_samples_of_2_gib(ee):
+    """Up to the last number of pixels: what a sample spans is counted in 64 bits."""
+    lib, n = ee.raw(), C.c_int64(-1)
+    for pixels in (1 << 30, (1 << 31) - 1024, (1 << 31) - 500, (1 << 31) - 1):
+        d = norm(ee, b=1, pixels=pixels, c=1, groups=1, x_sample=pixels, x_pixel=1, res_pixel=1, y_sample=pixels, y_pixel=1)
+        assert lib.ee_group_norm_workspace(C.byref(d), C.byref(n)) == ee.EE_ERR_OVERFLOW, pixels
+        assert lib.ee_group_norm(C.byref(d), P, None, None, None, P, P, 1 << 40, None) == ee.EE_ERR_OVERFLOW, pixels
