@@ -401,6 +401,13 @@ def _need(ok, what, code=EE_ERR_ARG):
         raise e
 
 
+def _int32(n, what):
+    """n for an int32 of the library's: ctypes would cut its upper bits off without a word."""
+    n = index(n)
+    _need(-1 << 31 <= n < 1 << 31, f"{what} do not fit 32 bits", EE_ERR_OVERFLOW)
+    return n
+
+
 # torch.cuda.current_stream() builds an object for this number: 2.6 us of a call of 8
 _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
@@ -481,7 +488,8 @@ def _norm_plan(x, out, residual, weight, bias, groups, eps, act, frac_bits, res_
     for t, name in ((weight, "weight"), (bias, "bias")):
         _need(t is None or t[0] == (c,) and (c == 1 or t[1] == (1,)), f"{name} has to be dense [channels]")
     _need(act in ACTS, f"act has to be one of {', '.join(ACTS)}")
-    d = NormDesc(EE_I8 if x[2] == torch.int8 else EE_BF16, ACTS[act], b, pixels, c, groups, frac_bits, res_shift, eps, 0, sample, pixel, r[3], r[4], y[3], y[4])
+    ints = [_int32(n, "sizes") for n in (b, pixels, c, groups, frac_bits, res_shift)]
+    d = NormDesc(EE_I8 if x[2] == torch.int8 else EE_BF16, ACTS[act], *ints, eps, 0, sample, pixel, r[3], r[4], y[3], y[4])
     need = C.c_int64()
     _chk(_lib.ee_group_norm_workspace(C.byref(d), C.byref(need)))
     return dev, C.byref(d), need.value
@@ -516,9 +524,10 @@ def _adapter_plan(dev, ci, co, adapters, rank, dtype, x, ids, offsets, out):
         _need(out[0] == x[0][:-1] + (co,), "out has to have the shape of x with co channels")
         ldy = _rows(out[0], out[1], "out")[3]
         _need(b * inner <= 1 or ldy >= co, "the rows of out must not share elements")
+    rows = _int32(b * inner, "rows")
     dims, need = AdapterDims(ci, co, adapters, rank), C.c_int64()
-    _chk(_lib.ee_adapter_workspace(C.byref(dims), b * inner, C.byref(need)))
-    return b * inner, slots, per, ldx, ldy, need.value
+    _chk(_lib.ee_adapter_workspace(C.byref(dims), rows, C.byref(need)))
+    return rows, _int32(slots, "slots"), _int32(per, "rows"), ldx, ldy, need.value
 
 
 class AdapterProjection:
@@ -533,7 +542,8 @@ class AdapterProjection:
         if bias is not None:
             _check(_key(bias), "bias", (torch.float32,), at)
             _need(bias.shape == (co,) and bias.is_contiguous(), "bias has to be dense [co]")
-        self.device, self.ci, self.co, self.adapters, self.rank = dev, ci, co, adapters, rank
+        adapters, rank = _int32(adapters, "adapters"), _int32(rank, "ranks")
+        self.device, self.ci, self.co, self.adapters, self.rank = dev, _int32(ci, "columns"), _int32(co, "outputs"), adapters, rank
         self._dims = AdapterDims(ci, co, adapters, rank)
         packed, pool = C.c_int64(), C.c_int64()
         _chk(_lib.ee_adapter_bytes(C.byref(self._dims), C.byref(packed), C.byref(pool)))
@@ -547,13 +557,13 @@ class AdapterProjection:
         _check(ka, "a", (torch.bfloat16,), at)
         _check(kb, "b", (torch.bfloat16,), at)
         _need(len(ka[0]) == 2 and len(kb[0]) == 2, "a has to be [r, ci] and b [co, r]")
-        r = ka[0][0]
+        r = _int32(ka[0][0], "ranks")
         _need(ka[0] == (r, self.ci) and kb[0] == (self.co, r), "a has to be [r, ci] and b [co, r]")
         _need((ka[1][1] == 1 or self.ci == 1) and (kb[1][1] == 1 or r == 1), "a and b have to have dense rows")
-        _on(at, _lib.ee_adapter_load, C.byref(self._dims), i, r, a.data_ptr(), ka[1][0] if r > 1 else self.ci, b.data_ptr(), kb[1][0] if self.co > 1 else r, scale, self._pool.data_ptr())
+        _on(at, _lib.ee_adapter_load, C.byref(self._dims), _int32(i, "adapters"), r, a.data_ptr(), ka[1][0] if r > 1 else self.ci, b.data_ptr(), kb[1][0] if self.co > 1 else r, scale, self._pool.data_ptr())
 
     def unload(self, i):
-        _on(self.device.index, _lib.ee_adapter_load, C.byref(self._dims), i, 0, None, 0, None, 0, 0.0, self._pool.data_ptr())
+        _on(self.device.index, _lib.ee_adapter_load, C.byref(self._dims), _int32(i, "adapters"), 0, None, 0, None, 0, 0.0, self._pool.data_ptr())
 
     def __call__(self, x, ids=None, offsets=None, out=None, dtype=torch.bfloat16):
         """x: bfloat16 [slots, ..., ci] or, with offsets (int32 [slots + 1]), [rows, ci] with the rows of slot s at offsets[s]..offsets[s + 1]; ids: int32 [slots], the adapter of
@@ -585,6 +595,7 @@ def _verify_plan(p, draft, u, q, lengths):
     _need(dense(p) and dense(draft) and dense(u), "the last dimension has to be dense")
     _need(q is None or q[0] == (b, k, v) and dense(q), "draft_probs has to be [b, k, v] with dense rows")
     _need(lengths is None or lengths[0] == (b,) and (b <= 1 or lengths[1] == (1,)), "lengths has to be dense [b]")
+    b, k, v = _int32(b, "sequences"), _int32(k, "drafts"), _int32(v, "tokens")
     need = C.c_int64()
     _chk(_lib.ee_verify_workspace(b, k, v, C.byref(need)))
     return dev, b, k, v, (draft[1][0], u[1][0], p[1][0], p[1][1]) + ((0, 0) if q is None else q[1][:2]), need.value

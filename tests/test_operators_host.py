@@ -130,3 +130,32 @@ def test_group_norm_refuses_samples_of_2_gib(ee):
         d = norm(ee, b=1, pixels=pixels, c=1, groups=1, x_sample=pixels, x_pixel=1, res_pixel=1, y_sample=pixels, y_pixel=1)
         assert lib.ee_group_norm_workspace(C.byref(d), C.byref(n)) == ee.EE_ERR_OVERFLOW, pixels
         assert lib.ee_group_norm(C.byref(d), P, None, None, None, P, P, 1 << 40, None) == ee.EE_ERR_OVERFLOW, pixels
+
+
+def test_binding_refuses_sizes_past_32_bits(ee):
+    """Sizes, numbers of adapters and places that an int32 cannot hold, of tensors that a GPU's memory may hold: refused, not cut down to what their lower bits say."""
+    import torch
+    big, key = 1 << 32, lambda shape, dtype=torch.bfloat16: (shape, tuple(torch.Size(shape[i + 1:]).numel() for i in range(len(shape))), dtype, 0)
+
+    def refused(f, *a):
+        with pytest.raises(ee.EEError) as e:
+            f(*a)
+        assert e.value.code == ee.EE_ERR_OVERFLOW
+    plan = lambda x, groups=4, frac=0, rs=0: ee._norm_plan(x, None, None, None, None, groups, 1e-5, "none", frac, rs)
+    assert plan(key((5, 7, 8)))[0] == 0
+    for call in [(key((big + 5, 1, 8)),), (key((1, big + 7, 8)),), (key((1, 1, big + 8)),), (key((5, 7, 8)), big + 4), (key((5, 7, 8)), 4 - big), (key((5, 7, 8)), 4, big), (key((5, 7, 8)), 4, 0, -big)]:
+        refused(plan, *call)
+    project = lambda x, ids, offsets=None: ee._adapter_plan(0, 8, 16, 2, 4, torch.bfloat16, x, ids, offsets, None)
+    ints = torch.int32
+    assert project(key((5, 8)), key((5,), ints))[0] == 5
+    refused(project, key((big + 5, 8)), key((big + 5,), ints))
+    refused(project, key((3, big, 8)), key((3,), ints))
+    refused(project, key((5, 8)), key((big + 1,), ints), key((big + 2,), ints))
+    verify = lambda b, k, v: ee._verify_plan(key((b, k + 1, v), torch.float32), key((b, k), ints), key((b, k + 1), torch.float32), None, None)
+    assert verify(2, 3, 9)[1:4] == (2, 3, 9)
+    for sizes in [(big + 2, 3, 9), (2, big + 3, 9), (2, 3, big + 9)]:
+        refused(verify, *sizes)
+    held = object.__new__(ee.AdapterProjection)                       # a handle without device memory
+    held.device, held.ci, held.co, held._dims, held._pool = torch.device("cuda", 0), 8, 16, ee.AdapterDims(8, 16, 2, 4), torch.zeros(1)
+    refused(held.unload, big)
+    refused(held.unload, big + 1)
