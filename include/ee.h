@@ -361,7 +361,8 @@ int ee_group_norm(const ee_norm_desc* desc, const void* x, const float* weight, 
  * A call: `rows` rows, `ldx` / `ldy` apart, belong to `slots` slots: `per` rows each (rows = slots * per), or, with offsets (device int32[slots + 1], not decreasing, per is not used), rows
  * [offsets[s], offsets[s + 1]) to slot s; rows in front of offsets[0] or from offsets[slots] on belong to none: they are left as they were in y, and what x holds there does not matter.
  * ids: device int32[slots], the slot's adapter; outside [0, adapters): none.  It may be NULL when adapters = 0.
- * EE_ERR_ARG: NULL or misaligned pointers, rows != slots * per, ldx < ci, ldy < co;  EE_ERR_OVERFLOW: ci or co above 2^18, rank above 256, adapters above 65536, rows above 2^22, too small a workspace. */
+ * y must not overlap x, not even where it is x: a row's results are written while others still read it.  Rows of both may take turns in one wider tensor (strides of the same number of bytes).
+ * EE_ERR_ARG: NULL or misaligned pointers, rows != slots * per, ldx < ci, ldy < co, y overlaps x;  EE_ERR_OVERFLOW: ci or co above 2^18, rank above 256, adapters above 65536, rows above 2^22, too small a workspace. */
 typedef struct { int32_t ci, co, adapters, rank; } ee_adapter_dims;
 typedef struct {
     const void* packed; const void* pool; const void* x; void* y; const int32_t* ids; const int32_t* offsets;

@@ -567,7 +567,8 @@ class AdapterProjection:
 
     def __call__(self, x, ids=None, offsets=None, out=None, dtype=torch.bfloat16):
         """x: bfloat16 [slots, ..., ci] or, with offsets (int32 [slots + 1]), [rows, ci] with the rows of slot s at offsets[s]..offsets[s + 1]; ids: int32 [slots], the adapter of
-        every slot, outside [0, adapters): none.  Returns bfloat16 or float32 (dtype) with co in place of ci."""
+        every slot, outside [0, adapters): none.  Returns bfloat16 or float32 (dtype) with co in place of ci; out must not overlap x.  Rows that belong to no slot are left as they were
+        in out; where out is not given they hold whatever the new memory held."""
         dev = self.device.index
         rows, slots, per, ldx, ldy, need = _adapter_plan(dev, self.ci, self.co, self.adapters, self.rank, dtype, _key(x), _key(ids), _key(offsets), _key(out))
         if out is None:

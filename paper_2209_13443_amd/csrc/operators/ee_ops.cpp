@@ -1,4 +1,6 @@
 // The C ABI of the operators that need no context: argument checks in front of their launches.
+#include <algorithm>
+
 #include "../ee_internal.hpp"
 
 using namespace ee;
@@ -7,6 +9,28 @@ namespace {
 
 bool aligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 int done(hipError_t e) { return e == hipSuccess ? EE_OK : EE_ERR_DEVICE; }
+
+// Elements [samples][pixels][channels], strides and the channels' size in bytes
+struct Elements { uintptr_t at; int64_t sample, pixel, channels; };
+
+// Whether no byte belongs to both: they lie one behind the other, or take turns -- pixel by pixel (channel slices of one wider tensor) or sample by sample
+bool apart(const Elements& p, const Elements& q, int64_t samples, int64_t pixels)
+{
+    typedef __int128 wide;
+    auto first = [&](const Elements& e) { return (wide)e.at + std::min<wide>(0, (wide)(samples - 1) * e.sample); };
+    auto extent = [&](const Elements& e) { return (wide)(samples - 1) * (e.sample < 0 ? -(wide)e.sample : e.sample) + (wide)(pixels - 1) * e.pixel + e.channels; };
+    if (first(p) + extent(p) <= first(q) || first(q) + extent(q) <= first(p)) return true;
+    // windows of lp and lq bytes, repeated every `pitch` bytes
+    auto turns = [&](wide pitch, wide lp, wide lq) {
+        const wide d = ((first(q) - first(p)) % pitch + pitch) % pitch;
+        return d >= lp && d + lq <= pitch;
+    };
+    // what the samples take up of a pixel's pitch: one place, or places next to one another
+    auto window = [&](const Elements& e) { return samples == 1 || e.sample % e.pixel == 0 ? (wide)e.channels : extent(e) - (wide)(pixels - 1) * e.pixel; };
+    if (pixels > 1 && p.pixel == q.pixel && p.pixel > 0 && turns(p.pixel, window(p), window(q))) return true;
+    const wide sample = p.sample < 0 ? -(wide)p.sample : p.sample;
+    return samples > 1 && p.sample == q.sample && sample > 0 && turns(sample, (wide)(pixels - 1) * p.pixel + p.channels, (wide)(pixels - 1) * q.pixel + q.channels);
+}
 
 int check_norm(const ee_norm_desc* d, NormArgs& a)
 {
@@ -118,6 +142,7 @@ extern "C" int ee_adapter_project(const ee_adapter_dims* dims, const ee_adapter_
     if (d.adapters > 0 && (!q.pool || !q.ids || !aligned(q.pool, 256))) return EE_ERR_ARG;
     if (!aligned(q.ids, 4) || !aligned(q.offsets, 4) || !q.workspace || !aligned(q.workspace, 256)) return EE_ERR_ARG;
     if (q.workspace_bytes < adapter_workspace(d, q.rows)) return EE_ERR_OVERFLOW;
+    if (!apart({(uintptr_t)q.x, 0, 2 * q.ldx, 2ll * d.ci}, {(uintptr_t)q.y, 0, (q.out_f32 ? 4 : 2) * q.ldy, (q.out_f32 ? 4ll : 2ll) * d.co}, 1, q.rows)) return EE_ERR_ARG;
     AdapterCall c{q.packed, q.pool, q.x, q.y, q.workspace, q.ids, q.offsets, q.ldx, q.ldy, q.rows, q.slots, q.per, q.out_f32};
     return done(launch_adapter_project(d, c, static_cast<hipStream_t>(hip_stream)));
 }

@@ -940,3 +940,27 @@ def test_adapter_projection_copies_more_elements_than_a_launch_has_threads(torch
         part = slice(first, first + (1 << 14))
         ref, tol = project_ref(torch, x[part], w, None, ad, ids[part], "fp32")
         assert bool(((got[part].double() - ref).abs() <= tol).all()), first
+
+
+def test_adapter_projection_next_to_its_input(torch, ee):
+    """Results in front of, behind and beside the rows they are of, in one tensor; over them they are refused."""
+    g = torch.Generator(device="cuda").manual_seed(41)
+    ci = co = 64
+    proj = ee.AdapterProjection((torch.randn(co, ci, device="cuda", generator=g) / 8).bfloat16())
+    x = torch.randn(700, ci, device="cuda", generator=g).bfloat16()
+    for rows in (1, 12, 700):
+        for dtype in (torch.bfloat16, torch.float32):
+            want = proj(x[:rows], dtype=dtype)
+            wide = torch.zeros(2 * rows, 3 * ci, device="cuda", dtype=torch.bfloat16)
+            n = 1 if dtype == torch.bfloat16 else 2
+            results = lambda t: t if n == 1 else t.view(dtype)
+            for src, dst in ((wide[:rows, :ci], wide[:rows, ci:ci + n * co]), (wide[:rows, 2 * ci:], wide[:rows, :n * co]), (wide[:rows, :ci], wide[rows:, :n * co]), (wide[rows:, ci:2 * ci], wide[:rows, ci:ci + n * co])):
+                src.copy_(x[:rows])
+                say(f"[case] {rows} rows {dtype}")
+                assert torch.equal(proj(src, out=results(dst), dtype=dtype), want)
+                assert torch.equal(src, x[:rows])
+            src = wide[:rows, :ci]
+            for dst in (wide[:rows, :n * co], wide[:rows, ci // 2:ci // 2 + n * co]):
+                with pytest.raises(ee.EEError) as e:
+                    proj(src, out=results(dst), dtype=dtype)
+                assert e.value.code == ee.EE_ERR_ARG

@@ -159,3 +159,20 @@ def test_binding_refuses_sizes_past_32_bits(ee):
     held.device, held.ci, held.co, held._dims, held._pool = torch.device("cuda", 0), 8, 16, ee.AdapterDims(8, 16, 2, 4), torch.zeros(1)
     refused(held.unload, big)
     refused(held.unload, big + 1)
+
+
+def test_adapter_projection_refuses_results_over_its_input(ee):
+    lib, n = ee.raw(), C.c_int64(-1)
+    d = ee.AdapterDims(64, 64, 0, 0)
+    assert lib.ee_adapter_workspace(C.byref(d), 12, C.byref(n)) == ee.EE_OK
+    x = 1 << 20
+
+    def call(y, **k):
+        c = dict(packed=P, pool=None, x=x, y=y, ids=None, offsets=None, ldx=64, ldy=64, rows=12, slots=12, per=1, out_f32=0, workspace=P, workspace_bytes=n.value)
+        c.update(k)
+        return lib.ee_adapter_project(C.byref(d), C.byref(ee.AdapterCall(**c)), None)
+    last = 2 * (11 * 64 + 64)                                             # bytes of x
+    for bad in [dict(y=x), dict(y=x + 2), dict(y=x - 2), dict(y=x + last - 2), dict(y=x - last + 2), dict(y=x, out_f32=1), dict(y=x - 2 * last + 4, out_f32=1), dict(y=x + 64, ldx=128, ldy=128),
+                dict(y=x - 130, ldx=192, ldy=192, rows=1, slots=1, per=1, x=x - 4), dict(y=x + 128, ldx=127, ldy=127), dict(y=x + 128, ldx=128, ldy=192), dict(y=x + 128, ldx=128, ldy=96, out_f32=1),
+                dict(y=x, rows=1, slots=1), dict(y=x + 126, rows=1, slots=1, ldx=4096, ldy=4096)]:
+        assert call(**bad) == ee.EE_ERR_ARG, bad
