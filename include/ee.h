@@ -339,8 +339,8 @@ enum { EE_ACT_NONE = 0, EE_ACT_RELU = 1, EE_ACT_RELU6 = 2, EE_ACT_SILU = 3 };
  *   int8  y = clamp(floor(d m + (bias 2^frac_bits + 1/2) + res 2^res_shift), lo, hi) with d = n x - sum x (exact) and
  *         m = weight 2^frac_bits / (n sqrt(var + eps)), in 64-bit floats, every operation rounded by itself (var: (n sum x^2 - (sum x)^2) / n^2); [lo, hi] = [-128, 127], with RELU [0, 127], with RELU6 [0, min(127, 6 * 2^frac_bits)]
  * weight, bias   device float[c], or NULL (1, 0);  res   device, the shape and type of x, added in front of the activation, or NULL
- * A group without variance and eps 0 is NaN; int8: lo for a NaN.  y may be x or res with its strides; otherwise it must not overlap them.  Samples of y must not share elements.  b == 0 or pixels == 0 is a no-op.
- * EE_ERR_ARG: c not a multiple of groups, pixel strides below 0 or, of y, below c, eps < 0 or not finite, frac_bits outside 0..7, res_shift outside -8..8, unknown act;  EE_ERR_UNSUPPORTED: SILU with int8, a group of more than
+ * A group without variance and eps 0 is NaN; int8: lo for a NaN.  y may be x or res with its strides; otherwise it must not overlap them (slices of one tensor may take turns).  Samples of y must not share elements.  b == 0 or pixels == 0 is a no-op.
+ * EE_ERR_ARG: c not a multiple of groups, pixel strides below 0 or, of y, below c, y over a part of x or res, eps < 0 or not finite, frac_bits outside 0..7, res_shift outside -8..8, unknown act;  EE_ERR_UNSUPPORTED: SILU with int8, a group of more than
  * 1024 channels (8192 where they are whole 16-byte pieces and x, y, res and their strides are 16-byte aligned);  EE_ERR_OVERFLOW: int8 groups of 2^24 values or more, a sample that spans 2 GiB less 1024 pixels or more, a pixel stride of 2^20 or more, too small a workspace. */
 typedef struct {
     int32_t dtype, act, b, pixels, c, groups, frac_bits, res_shift;

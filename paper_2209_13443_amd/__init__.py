@@ -497,7 +497,8 @@ def _norm_plan(x, out, residual, weight, bias, groups, eps, act, frac_bits, res_
 
 def group_norm(x, groups, weight=None, bias=None, eps=1e-5, act="none", residual=None, frac_bits=0, res_shift=0, out=None):
     """ee_group_norm: act(group norm of x + residual) on x[b, ..., c] (int8, bfloat16 or int16 holding bf16 bits; any sample stride, one pixel stride, channel slices included).
-    weight, bias: float32 [c].  act: "none", "relu", "relu6", "silu" (not int8).  int8: the result is in units of 2^-frac_bits, the residual enters times 2^res_shift."""
+    weight, bias: float32 [c].  act: "none", "relu", "relu6", "silu" (not int8).  int8: the result is in units of 2^-frac_bits, the residual enters times 2^res_shift.
+    out may be x or residual, or share nothing with them."""
     dev, desc, need = _norm_plan(_key(x), _key(out), _key(residual), _key(weight), _key(bias), index(groups), float(eps), act, index(frac_bits), index(res_shift))
     if out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)

@@ -81,14 +81,19 @@ extern "C" int ee_group_norm(const ee_norm_desc* desc, const void* x, const floa
     NormArgs a;
     if (const int rc = check_norm(desc, a)) return rc;
     if (a.b == 0 || a.pixels == 0) return EE_OK;
-    const unsigned es = a.dtype == EE_I8 ? 1 : 2;
-    if (!x || !y || !aligned(x, es) || !aligned(y, es) || !aligned(res, es) || !aligned(weight, 4) || !aligned(bias, 4)) return EE_ERR_ARG;
+    const int64_t es = a.dtype == EE_I8 ? 1 : 2;
+    if (!x || !y || !aligned(x, (unsigned)es) || !aligned(y, (unsigned)es) || !aligned(res, (unsigned)es) || !aligned(weight, 4) || !aligned(bias, 4)) return EE_ERR_ARG;
     a.x = x; a.res = res; a.y = y; a.weight = weight; a.bias = bias;
     if (!group_norm_supported(a)) return EE_ERR_UNSUPPORTED;
     const size_t need = group_norm_workspace(a);
     if (need && (!workspace || !aligned(workspace, 256))) return EE_ERR_ARG;
     if (workspace_bytes < (int64_t)need) return EE_ERR_OVERFLOW;
     if (!group_norm_grid_fits(a)) return EE_ERR_OVERFLOW;
+    // y is x, or res, or shares nothing with it
+    auto elements = [&](const void* at, int64_t sample, int64_t pixel) { return Elements{(uintptr_t)at, a.b == 1 ? 0 : es * sample, a.pixels == 1 ? 0 : es * pixel, (int64_t)es * a.c}; };
+    const Elements of_y = elements(y, a.y_sample, a.y_pixel);
+    for (const Elements& e : {elements(x, a.x_sample, a.x_pixel), res ? elements(res, a.res_sample, a.res_pixel) : of_y})
+        if (!(e.at == of_y.at && e.sample == of_y.sample && e.pixel == of_y.pixel) && !apart(e, of_y, a.b, a.pixels)) return EE_ERR_ARG;
     return done(launch_group_norm(a, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 

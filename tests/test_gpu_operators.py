@@ -964,3 +964,31 @@ def test_adapter_projection_next_to_its_input(torch, ee):
                 with pytest.raises(ee.EEError) as e:
                     proj(src, out=results(dst), dtype=dtype)
                 assert e.value.code == ee.EE_ERR_ARG
+
+
+def test_group_norm_next_to_its_input(torch, ee):
+    """Results beside, between, in front of and behind what they are of, in one tensor, or over it; over a part of it they are refused."""
+    g = torch.Generator(device="cuda").manual_seed(42)
+    for b, p, c in ((1, 1, 32), (3, 1, 32), (1, 20, 32), (3, 20, 32), (2, 5000, 32), (2, 20, 33)):
+        x0, r0 = ((torch.randn(b, p, c, device="cuda", generator=g) * 3).bfloat16() for _ in range(2))
+        groups = c // 8 if c % 8 == 0 else 3
+        plain, with_res = ee.group_norm(x0, groups, act="relu"), ee.group_norm(x0, groups, act="relu", residual=r0)
+        new = lambda *s: torch.zeros(s, device="cuda", dtype=torch.bfloat16)
+        wide, samples, turns, line = new(b, p, 3 * c), new(3 * b, p, c), new(p, 3 * b, c), new(3, b, p, c)
+        for views in ([wide[..., i * c:(i + 1) * c] for i in range(3)], [samples[i::3] for i in range(3)], [samples[i * b:(i + 1) * b] for i in range(3)], [turns[:, i * b:(i + 1) * b].transpose(0, 1) for i in range(3)],
+                      [turns[:, i::3].transpose(0, 1) for i in range(3)] if b == 1 else [line[i] for i in range(3)]):
+            for i, j, k in ((0, 1, 2), (2, 0, 1), (1, 2, 0)):
+                x, out, res = views[i], views[j], views[k]
+                x.copy_(x0)
+                res.copy_(r0)
+                say(f"[case] {b} x {p} x {c}")
+                near = lambda a, w: bool(((a.double() - w.double()).abs() <= 2.0 ** -6 * w.double().abs() + 2.0 ** -14).all())      # alignment chooses the order of sums
+                assert near(ee.group_norm(x, groups, act="relu", out=out), plain) and near(ee.group_norm(x, groups, act="relu", residual=res, out=out), with_res)
+                assert torch.equal(x, x0) and torch.equal(res, r0)
+                assert near(ee.group_norm(x, groups, act="relu", residual=res, out=res), with_res) and torch.equal(x, x0)
+                assert near(ee.group_norm(x, groups, act="relu", out=x), plain)
+        flat = new(b * p * c + c)
+        for at in (1, 8, c):
+            with pytest.raises(ee.EEError) as e:
+                ee.group_norm(flat[:b * p * c].view(b, p, c), groups, out=flat[at:at + b * p * c].view(b, p, c)) if b * p * c > at else ee.group_norm(flat[:c].view(1, 1, c), groups, out=flat[1:1 + c].view(1, 1, c))
+            assert e.value.code == ee.EE_ERR_ARG

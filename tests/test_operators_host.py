@@ -176,3 +176,16 @@ def test_adapter_projection_refuses_results_over_its_input(ee):
                 dict(y=x - 130, ldx=192, ldy=192, rows=1, slots=1, per=1, x=x - 4), dict(y=x + 128, ldx=127, ldy=127), dict(y=x + 128, ldx=128, ldy=192), dict(y=x + 128, ldx=128, ldy=96, out_f32=1),
                 dict(y=x, rows=1, slots=1), dict(y=x + 126, rows=1, slots=1, ldx=4096, ldy=4096)]:
         assert call(**bad) == ee.EE_ERR_ARG, bad
+
+
+def test_group_norm_refuses_results_over_a_part_of_its_input(ee):
+    lib, n = ee.raw(), C.c_int64(-1)
+    x = 1 << 20
+    whole = 2 * 2 * 49 * 64                                               # bytes of a dense x
+    for k, y, res in [({}, x + 2, None), ({}, x - 2, None), ({}, x + 2 * 64, None), ({}, x + whole - 2, None), ({}, x - whole + 2, None), ({}, x - whole, x - 2), ({}, x + 2 * whole, x + 2 * whole + 16),
+                      (dict(y_pixel=96, y_sample=49 * 96), x, None), (dict(x_pixel=128, y_pixel=128, x_sample=49 * 128, y_sample=49 * 128), x + 64, None),
+                      (dict(x_sample=49 * 64, y_sample=2 * 49 * 64), x, None), (dict(x_sample=0), x, None), (dict(pixels=1, x_sample=64, y_sample=128), x, None), (dict(b=1), x + 2, None)]:
+        d = norm(ee, res_sample=49 * 64, res_pixel=64)
+        for name, v in k.items():
+            setattr(d, name, v)
+        assert lib.ee_group_norm(C.byref(d), x, None, None, res, y, None, 0, None) == ee.EE_ERR_ARG, (k, y, res)
