@@ -992,3 +992,39 @@ def test_group_norm_next_to_its_input(torch, ee):
             with pytest.raises(ee.EEError) as e:
                 ee.group_norm(flat[:b * p * c].view(b, p, c), groups, out=flat[at:at + b * p * c].view(b, p, c)) if b * p * c > at else ee.group_norm(flat[:c].view(1, 1, c), groups, out=flat[1:1 + c].view(1, 1, c))
             assert e.value.code == ee.EE_ERR_ARG
+
+
+@pytest.mark.parametrize("slots,per,ci,co,r,n", [(40, 127, 1096, 250, 32, 5), (64, 196, 1024, 256, 32, 16), (3, 5000, 40, 129, 8, 5), (24, 255, 1032, 1000, 32, 5), (12, 1, 4096, 4096, 16, 8), (64, 1, 2048, 1000, 16, 24),
+                                                 (300, 1, 2048, 512, 16, 24), (200, 7, 1096, 1000, 64, 9), (24, 333, 4096, 4096, 64, 16)])
+def test_adapter_projection_repeats_its_bits(torch, ee, slots, per, ci, co, r, n):
+    """The same call gives the same bits, of infinities and NaN too, with other work in the caches between the calls."""
+    g = torch.Generator(device="cuda").manual_seed(slots + co)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    say(f"[case] {slots} x {per} {ci} -> {co} rank {r}")
+    proj = ee.AdapterProjection((rnd(co, ci) / ci ** 0.5).bfloat16(), rnd(co), adapters=n, rank=r)
+    for i, (a, b, s) in enumerate(adapters_of(torch, g, n, r, ci, co)):
+        if i == n - 1:
+            b[co // 2, 0] = float("inf")
+        proj.load(i, a, b, s)
+    ids = torch.randint(-1, n, (slots,), device="cuda", generator=g, dtype=torch.int32)
+    ids[0] = n - 1
+    x = rnd(slots, per, ci).bfloat16()
+    for dtype, bits in ((torch.bfloat16, torch.int16), (torch.float32, torch.int32)):
+        first = proj(x, ids, dtype=dtype)
+        for turn in range(6):
+            other = torch.full((1 << (18 + turn),), float(turn), device="cuda")
+            assert torch.equal(proj(x, ids, dtype=dtype).view(bits), first.view(bits)), turn
+            assert bool((other == turn).all())
+
+
+@pytest.mark.parametrize("b,p,c,groups", [(1, 49, 512, 32), (64, 3136, 256, 32), (37, 1225, 96, 12), (2, 40000, 64, 32), (9, 400, 33, 3)])
+def test_group_norm_repeats_its_bits(torch, ee, b, p, c, groups):
+    g = torch.Generator(device="cuda").manual_seed(p)
+    x = (torch.randn(b, p, c, device="cuda", generator=g) * 3 + 1).bfloat16()
+    x[0, 0, 0] = float("nan")
+    say(f"[case] {b} x {p} x {c}")
+    first = ee.group_norm(x, groups, act="silu", residual=x)
+    for turn in range(6):
+        other = torch.full((1 << (18 + turn),), float(turn), device="cuda")
+        assert torch.equal(ee.group_norm(x, groups, act="silu", residual=x).view(torch.int16), first.view(torch.int16)), turn
+        assert bool((other == turn).all())
