@@ -335,7 +335,7 @@ enum { EE_ACT_NONE = 0, EE_ACT_RELU = 1, EE_ACT_RELU6 = 2, EE_ACT_SILU = 3 };
 
 /* Group norm with an activation, channels last.  x[b][pixels][c] (int8 or bf16), channels are neighbours, sample and pixel strides are free: a channel slice of a wider tensor is one.
  * Group g of a sample is channels [g c / groups, (g + 1) c / groups) of all its pixels, n values; var is their variance (divided by n).
- *   bf16  y = act(weight (x - mean) / sqrt(var + eps) + bias + res), computed in float and rounded once; a NaN in a group makes the group NaN
+ *   bf16  y = act(weight (x - mean) / sqrt(var + eps) + bias + res), computed in float and rounded once (the order of the statistics' sums goes with b); a NaN in a group makes the group NaN
  *   int8  y = clamp(floor(d m + (bias 2^frac_bits + 1/2) + res 2^res_shift), lo, hi) with d = n x - sum x (exact) and
  *         m = weight 2^frac_bits / (n sqrt(var + eps)), in 64-bit floats, every operation rounded by itself (var: (n sum x^2 - (sum x)^2) / n^2); [lo, hi] = [-128, 127], with RELU [0, 127], with RELU6 [0, min(127, 6 * 2^frac_bits)]
  * weight, bias   device float[c], or NULL (1, 0);  res   device, the shape and type of x, added in front of the activation, or NULL
@@ -353,7 +353,8 @@ int ee_group_norm(const ee_norm_desc* desc, const void* x, const float* weight, 
 
 /* A shared projection with each request's low-rank adapter beside it (bf16): for every row m of x, with a the adapter of its slot,
  *   y[m][o] = sum_c x[m][c] w[o][c] + bias[o] + scale_a sum_r b_a[o][r] (sum_c a_a[r][c] x[m][c])
- * Sums are in float; the inner one is rounded to 2^-18 relative for bf16 results, to 2^-24 for float ones.  y is bf16 or float.
+ * Sums are in float; for bf16 results of more than a few rows the inner one is rounded to 2^-18 relative, else it stays a float.  y is bf16 or float.  The order of the sums, and so the last bits of a
+ * row, go with the sizes of the call and the adapters of the rows near it; the same call gives the same bits.
  * Infinities and NaN of an adapter or of a row of x reach the rows of that adapter, that row, and no others.
  * Weights are laid out once: ee_adapter_bytes sizes the two device buffers (256-byte aligned) a program keeps, ee_adapter_pack fills the first with w[co][ci] and bias (float[co] or
  * NULL), ee_adapter_load puts adapter i (a[rank][ci], b[co][rank], rank <= dims->rank) into the second, also between calls; rank 0 takes it out again (a, b may be NULL).  The second buffer
@@ -381,7 +382,7 @@ int ee_adapter_project(const ee_adapter_dims* dims, const ee_adapter_call* call,
  * p_n: the first j with w_0 + .. + w_j > u_k sum(w), or the last of positive weight.  Weights that are not finite and positive count as 0; if all are, the token is -1.
  *   lengths        device int32[b], or NULL: drafts of the sequence, at most k count; < 0: an empty slot (nothing accepted, all tokens -1)
  *   accepted[b]    device int32: drafts accepted;  tokens[b][k + 1] device int32: the accepted drafts, the drawn token, -1 behind it
- * p and q are float or bf16 (f32 = 1 or 0), entries of a row are neighbours.  The products and sums are in 64-bit floats, added in one order whatever else runs.  b == 0 is a no-op, k may be 0.
+ * p and q are float or bf16 (f32 = 1 or 0), entries of a row are neighbours.  The products and sums are in 64-bit floats, added in one order whatever else runs (it goes with b and v).  b == 0 is a no-op, k may be 0.
  * EE_ERR_ARG: NULL pointers, v < 1, b or k < 0;  EE_ERR_OVERFLOW: v above 2^30, b (k + 1) above 2^28, b of 2^23 or more, too small a workspace. */
 typedef struct {
     const int32_t* draft; const void* p; const void* q; const float* u; const int32_t* lengths; int32_t* accepted; int32_t* tokens;

@@ -2,8 +2,10 @@
 //
 //   y[m][o] = sum_c x[m][c] W[o][c] + bias[o] + sum_r B_a[o][r] u[m][r],   u[m][r] = scale_a sum_c A_a[r][c] x[m][c],   a: the adapter of row m, or none
 //
-// Two launches, or, for long slots and few outputs, one.  The first computes u (adapter_shrink_kernel) and the adapter of every row; u is kept as the sum of bf16 numbers (head and remainders:
-// two of them, relative error 2^-18, for bf16 results, three, 2^-26, for float ones), so that the second half of an adapter runs on the matrix cores as well; few rows keep it in float.  The second is the projection, with the adapters as
+// Two launches, or, for long slots and few outputs, one.  The first computes u (adapter_shrink_kernel) and the adapter of every row; u is kept as the sum of bf16 numbers, a head and remainders, so that
+// the second half of an adapter runs on the matrix cores as well: three of them for float results, which hold all of a float, two for bf16 results, relative error 2^-18.  That is a 1,024th of a result's own
+// rounding and, where terms cancel, what float sums of thousands of them lose as well; a third number for these too, us: 4096 -> 4096, 128 rows of 24 adapters of rank 16 32.7 / 38.0, 8,000 rows of rank 64 242 / 253, 12,544 rows
+// 1024 -> 256 of rank 32 21.0 / 21.7, 4,096 rows 1024 -> 1024 of 32 adapters 27.6 / 30.2.  Few rows keep u in float.  The second launch is the projection, with the adapters as
 // further steps of its reduction: for each adapter among a tile's rows, the rows of others read zeros.  A second half that has infinities or NaN, which zeros times it would give to the rows of
 // others, is no step: its own rows add it element by element.
 //
@@ -755,8 +757,9 @@ template <int MB, int NB, int WM, int WN, int KG, int RING, bool FUSE = false>
 hipError_t launch_form(const AdapterKernelArgs& k, hipStream_t s) { return k.out_f32 ? launch_tiles<MB, NB, WM, WN, KG, RING, true, FUSE>(k, s) : launch_tiles<MB, NB, WM, WN, KG, RING, false, FUSE>(k, s); }
 
 // Whether tiles compute the first halves themselves: slots as long as a tile, and outputs that few tiles share, or x would be multiplied with the first halves too often: one column of tiles, or one round
-// of tiles, two columns of them or a short reduction.  Both launches / this, us, rank 32: 12544 rows 1024 -> 128 24.3 / 20.1, -> 256 27.2 / 22.1, -> 512 34 / 38; 38400 rows 4096 -> 128 172 / 122,
-// -> 256 188 / 166, 1024 -> 256 50 / 54; 3136 rows 64 -> 1024 14.7 / 11.4, 512 -> 1024 16.5 / 15.2, 2048 -> 1024 29.9 / 29.9, 1024 -> 128 13.7 / 17.9
+// of tiles, two columns of them or a short reduction.  Both launches / this, us, rank 32: 12544 rows 1024 -> 128 24.3 / 20.1, -> 256 27.2 / 22.1, -> 512 34 / 38; 38400 rows 4096 -> 128 172 / 122;
+// 3136 rows 64 -> 1024 14.7 / 11.4, 512 -> 1024 16.5 / 15.2, 2048 -> 1024 29.9 / 29.9, 1024 -> 128 13.7 / 17.9.  Beyond one round two columns go either way with the reduction's length and are left to two
+// launches: 38400 rows 4096 -> 256 188 / 166, 1024 -> 256 50 / 54
 bool fused(const AdapterKernelArgs& k)
 {
     if (k.offsets || k.adapters == 0 || k.per < 127 || k.rp > 32) return false;

@@ -180,12 +180,11 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
         }
     };
 
-    constexpr int TV = NV;                                            // vectors a lane holds of x (two launches: of two sets)
-    raw data[TV];
+    raw data[NV];                                                     // two launches: one of two sets
     const bool has_res = FORM != 1 && a.res;
     const View<ES, VEC> res((const T*)a.res + b * a.r_sample + p0 * a.r_pixel + c0, a.r_pixel, has_res ? end - p0 : 0, cw, live, row, col);
 #pragma unroll
-    for (int i = 0; i < TV; ++i) data[i] = x.load(i * rows);         // pixels are counted from p0 from here on
+    for (int i = 0; i < NV; ++i) data[i] = x.load(i * rows);         // pixels are counted from p0 from here on
     const int count = end - p0, mine = p1 - p0;
     // the lane's channels' factors, loaded with the first pixels
     constexpr bool AFFINE = FORM != 1 && (ES == 2 || VEC == 1);
@@ -374,7 +373,7 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
     // f(x, residual) -> y for every vector of the lane, four at a time, the next four's residuals (FORM 2: and x) on their way
     auto tiles = [&](auto res_tag, auto&& f) {
         constexpr bool RES = decltype(res_tag)::value;
-        constexpr int BV = TV < 4 ? TV : 4;
+        constexpr int BV = NV < 4 ? NV : 4;
         raw r[2][BV], d2[BV];
         auto residuals = [&](raw (&to)[BV], int i0) {
             if constexpr (RES)
@@ -392,8 +391,8 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
         residuals(r[0], 0);
         if constexpr (FORM == 0) {
 #pragma unroll
-            for (int k = 0; k < TV / BV; ++k) {
-                if (k + 1 < TV / BV) residuals(r[(k + 1) & 1], (k + 1) * BV * rows);
+            for (int k = 0; k < NV / BV; ++k) {
+                if (k + 1 < NV / BV) residuals(r[(k + 1) & 1], (k + 1) * BV * rows);
                 four(data + k * BV, r[k & 1], k * BV * rows);
             }
         } else {
@@ -581,7 +580,7 @@ bool plan_norm_vec(const NormArgs& a, int vec, NormPlan& p)
     for (int want = 64; want >= 8; want /= 2) {
         window(want);
         p.nt = p.wlog > 8 ? 1024 : 256;
-        p.nv = 8;                                                     // in two sets
+        p.nv = 8;                                                     // the kernel's two sets of NV = 4
         if (!fits()) continue;
         const int tile = p.nv * (p.nt >> p.wlog);                     // pixels a workgroup holds at once
         const int64_t tiles = ((int64_t)a.pixels + tile - 1) / tile, units = (int64_t)a.b * p.windows;
