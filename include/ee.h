@@ -335,7 +335,7 @@ enum { EE_ACT_NONE = 0, EE_ACT_RELU = 1, EE_ACT_RELU6 = 2, EE_ACT_SILU = 3 };
 
 /* Group norm with an activation, channels last.  x[b][pixels][c] (int8 or bf16), channels are neighbours, sample and pixel strides are free: a channel slice of a wider tensor is one.
  * Group g of a sample is channels [g c / groups, (g + 1) c / groups) of all its pixels, n values; var is their variance (divided by n).
- *   bf16  y = act(weight (x - mean) / sqrt(var + eps) + bias + res), computed in float and rounded once (the order of the statistics' sums goes with b); a NaN in a group makes the group NaN
+ *   bf16  y = act(weight (x - mean) / sqrt(var + eps) + bias + res), computed in float and rounded once (the order of the statistics' sums goes with b); a NaN, an infinity or a deviation whose square passes float's range (1.8e19) in a group makes the group NaN
  *   int8  y = clamp(floor(d m + (bias 2^frac_bits + 1/2) + res 2^res_shift), lo, hi) with d = n x - sum x (exact) and
  *         m = weight 2^frac_bits / (n sqrt(var + eps)), in 64-bit floats, every operation rounded by itself (var: (n sum x^2 - (sum x)^2) / n^2); [lo, hi] = [-128, 127], with RELU [0, 127], with RELU6 [0, min(127, 6 * 2^frac_bits)]
  * weight, bias   device float[c], or NULL (1, 0);  res   device, the shape and type of x, added in front of the activation, or NULL

@@ -156,7 +156,7 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
     unsigned char* const l_group = (unsigned char*)(l_part + slices * cols * GPV);                   // per group: bf16 mean and 1 / deviation; int8 S1 and n deviation
     const double n_all = (double)a.pixels * a.cpg;
     auto settle = [&](int g, const stat_t& s) {
-        if constexpr (ES == 2) ((float2*)l_group)[g] = float2{s.mean, rsqrtf(s.m2 / (float)n_all + a.eps)};
+        if constexpr (ES == 2) ((float2*)l_group)[g] = float2{s.mean, rsqrtf(s.m2 / (float)n_all + a.eps) + 0.f * s.m2};      // squares past float's range: NaN, as those in a lane's own sums
         else {
             const long long n = (long long)a.pixels * a.cpg;
             const double var = (double)(n * s.s2 - (long long)s.s1 * s.s1) / (n_all * n_all);

@@ -1028,3 +1028,24 @@ def test_group_norm_repeats_its_bits(torch, ee, b, p, c, groups):
         other = torch.full((1 << (18 + turn),), float(turn), device="cuda")
         assert torch.equal(ee.group_norm(x, groups, act="silu", residual=x).view(torch.int16), first.view(torch.int16)), turn
         assert bool((other == turn).all())
+
+
+@pytest.mark.parametrize("h,w,c,groups", [(1, 1, 32, 4), (1, 2, 32, 4), (2, 2, 32, 32), (7, 7, 64, 8), (20, 20, 33, 3), (35, 35, 96, 12), (100, 101, 64, 32)])
+def test_group_norm_of_lowest_values(torch, ee, h, w, c, groups):
+    """A value whose deviation has no square in float, as masks have them: its group is NaN wherever it lies, never a bias that looks sound; the other groups are as they were."""
+    g = torch.Generator(device="cuda").manual_seed(h * c)
+    x = torch.randn(2, h, w, c, device="cuda", generator=g).bfloat16()
+    cpg = c // groups
+    bias = torch.ones(c, device="cuda")
+    clean = ee.group_norm(x, groups, None, bias)
+    for value in (torch.finfo(torch.bfloat16).min, torch.finfo(torch.bfloat16).max, float("inf"), -float("inf"), float("nan")):
+        for pixel in sorted({0, 1, h * w // 2, h * w - 1} & set(range(h * w))):
+            say(f"[case] {h}x{w}x{c} groups {groups} {value} at {pixel}")
+            bad = x.clone()
+            bad.view(2, h * w, c)[1, pixel, 2 * cpg] = value
+            got = ee.group_norm(bad, groups, None, bias)
+            mine = torch.zeros(2, h, w, c, dtype=torch.bool, device="cuda")
+            mine[1, :, :, 2 * cpg:3 * cpg] = True
+            if h * w * cpg > 1 or value != value or abs(value) == float("inf"):
+                assert bool(got[mine].isnan().all()), float(got[mine].float().abs().max())
+            assert torch.equal(got[~mine], clean[~mine])
