@@ -87,11 +87,11 @@ int pack_op(ee_ctx* ctx, const unsigned char* blob, OpPlan& p)
         p.weight_bytes = 8.0 * d.c_in;
         NormArgs probe = ctx->norm_args(p, 1);
         probe.y = reinterpret_cast<void*>((uintptr_t)d.c_off * es);  // the slice's place in its pixel, from an aligned tensor
-        if (!rc && !group_norm_supported(probe)) rc = EE_ERR_UNSUPPORTED;
+        if (!rc) rc = group_norm_check(probe);
         if (!rc && (d.c_tot >= 1 << 20 || (((int64_t)d.h_in * d.w_in + 1024) * d.c_tot + d.c_in) * es >= 1ll << 31)) rc = EE_ERR_OVERFLOW;      // the kernel's offsets
         for (int n = 1; n <= ctx->b_max && !rc; ++n) {               // how a call is cut up depends on the batch
             const NormArgs a = ctx->norm_args(p, n);
-            if (!group_norm_grid_fits(a)) rc = EE_ERR_OVERFLOW;
+            rc = group_norm_check(a);
             ctx->norm_ws_bytes = std::max(ctx->norm_ws_bytes, group_norm_workspace(a));
         }
         return rc;

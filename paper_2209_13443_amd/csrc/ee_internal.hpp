@@ -433,8 +433,7 @@ struct NormArgs {         // group norm with an activation; strides in elements,
     int dtype, act, b, pixels, c, groups, frac_bits, res_shift;
     float eps;
 };
-bool group_norm_supported(const NormArgs& a);           // a group's channels fit a workgroup's columns
-bool group_norm_grid_fits(const NormArgs& a);
+int group_norm_check(const NormArgs& a);                // EE_OK; EE_ERR_UNSUPPORTED: a group's channels do not fit a workgroup's columns; EE_ERR_OVERFLOW: a sample's workgroups do not fit a launch
 size_t group_norm_workspace(const NormArgs& a);
 hipError_t launch_group_norm(const NormArgs& a, void* workspace, hipStream_t s);
 

@@ -84,11 +84,10 @@ extern "C" int ee_group_norm(const ee_norm_desc* desc, const void* x, const floa
     const int64_t es = a.dtype == EE_I8 ? 1 : 2;
     if (!x || !y || !aligned(x, (unsigned)es) || !aligned(y, (unsigned)es) || !aligned(res, (unsigned)es) || !aligned(weight, 4) || !aligned(bias, 4)) return EE_ERR_ARG;
     a.x = x; a.res = res; a.y = y; a.weight = weight; a.bias = bias;
-    if (!group_norm_supported(a)) return EE_ERR_UNSUPPORTED;
+    if (const int rc = group_norm_check(a)) return rc;
     const size_t need = group_norm_workspace(a);
     if (need && (!workspace || !aligned(workspace, 256))) return EE_ERR_ARG;
     if (workspace_bytes < (int64_t)need) return EE_ERR_OVERFLOW;
-    if (!group_norm_grid_fits(a)) return EE_ERR_OVERFLOW;
     // y is x, or res, or shares nothing with it
     auto elements = [&](const void* at, int64_t sample, int64_t pixel) { return Elements{(uintptr_t)at, a.b == 1 ? 0 : es * sample, a.pixels == 1 ? 0 : es * pixel, (int64_t)es * a.c}; };
     const Elements of_y = elements(y, a.y_sample, a.y_pixel);

@@ -659,10 +659,11 @@ bool norm_aligned(const NormArgs& a)
 
 }  // namespace
 
-bool group_norm_supported(const NormArgs& a) { return plan_norm(a, norm_aligned(a)).ok; }
-
-// one sample does
-bool group_norm_grid_fits(const NormArgs& a) { return a.b == 0 || plan_norm(a, norm_aligned(a)).batch > 0; }
+int group_norm_check(const NormArgs& a)
+{
+    const NormPlan p = plan_norm(a, norm_aligned(a));
+    return !p.ok ? EE_ERR_UNSUPPORTED : p.batch < 1 ? EE_ERR_OVERFLOW : EE_OK;
+}
 
 // a call whose alignment is not known yet may be cut either way
 size_t group_norm_workspace(const NormArgs& a)
