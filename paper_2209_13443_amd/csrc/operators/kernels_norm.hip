@@ -639,9 +639,9 @@ hipError_t launch_norm_gpv(const NormKernelArgs& k, const NormPlan& p, hipStream
     }
     if (p.nt == 256) return p.nv == 1 ? launch_norm_form<ES, VEC, GPV, 256, 1, 0>(k, s) : launch_norm_form<ES, VEC, GPV, 256, 4, 0>(k, s);
     if (p.nt == 512) return launch_norm_form<ES, VEC, GPV, 512, 4, 0>(k, s);
-    // the partials of 1,024 threads with sixteen groups to a column (int8) are more than LDS holds: no plan has them
+    if (!p.split) return launch_norm_form<ES, VEC, GPV, 1024, 4, 0>(k, s);
+    // two launches of 1,024 threads are for windows of more than 256 columns, a partial of each group for every thread: with sixteen groups to a column (int8) more than LDS holds, so no plan has them
     if constexpr ((ES == 2 ? 8 : 16) * 1024 * GPV <= NORM_LDS) {
-        if (!p.split) return launch_norm_form<ES, VEC, GPV, 1024, 4, 0>(k, s);
         // int8's second launch keeps 16 to 20 registers in memory (128 are a thread's): 16 x 900x8192, groups of 8,192 channels 75 us, of 4,096, with 256 threads, 64
         const hipError_t e = launch_norm_form<ES, VEC, GPV, 1024, 4, 1>(k, s);
         timed.before(last);

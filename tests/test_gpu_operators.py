@@ -1049,3 +1049,18 @@ def test_group_norm_of_lowest_values(torch, ee, h, w, c, groups):
             if h * w * cpg > 1 or value != value or abs(value) == float("inf"):
                 assert bool(got[mine].isnan().all()), float(got[mine].float().abs().max())
             assert torch.equal(got[~mine], clean[~mine])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "int8"])
+@pytest.mark.parametrize("pixels", [300, 700, 1023, 1025, 1800, 2047, 2049, 2500, 4095, 4097])
+def test_group_norm_on_both_sides_of_every_form(torch, ee, dtype, pixels):
+    """Numbers of pixels around where 256, 512 and 1,024 threads hold a sample, groups of one channel, of three, of a column's sixteenth, fourth and whole, with few and with many samples."""
+    g = torch.Generator(device="cuda").manual_seed(pixels)
+    for c, groups in ((16, 16), (32, 32), (48, 16), (48, 48), (64, 16), (64, 8), (80, 8), (96, 3), (112, 7), (33, 11), (272, 16)):
+        for b in (1, 3, 90):
+            x = torch.randint(-100, 101, (b, pixels, c), device="cuda", generator=g, dtype=torch.int8)
+            x = x if dtype == "int8" else (x.float() / 7).bfloat16()
+            say(f"[case] {dtype} {b} x {pixels} x {c} groups {groups}")
+            ref, bound = norm_ref(torch, x, groups, None, None, 1e-5, "none", None, 5)
+            got = ee.group_norm(x, groups, frac_bits=5)
+            assert torch.equal(got, ref) if bound is None else bool(((got.double() - ref).abs() <= bound).all())
