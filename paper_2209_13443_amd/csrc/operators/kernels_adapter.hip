@@ -314,7 +314,8 @@ __global__ __launch_bounds__(512) void adapter_rows_project_kernel(AdapterKernel
         float v = bias;
 #pragma unroll
         for (int q = 0; q < NW; ++q) v += l_sum[q][row][tid & 15];
-        if (id[j] >= 0)
+        if (id[j] >= 0) {
+            float sum_b = 0.f;                                                   // by itself: up to 256 small terms, one by one onto a large v, would lose eight bits of theirs
             for (int r = 0; r < a.rp; r += 16) {
                 if (r) load_adapter(j, r);
                 float sum = uv[j][0];                                            // of element r + tid % 16; the row's sixteen threads show them to each other
@@ -323,10 +324,12 @@ __global__ __launch_bounds__(512) void adapter_rows_project_kernel(AdapterKernel
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const uint32_t two = (uint32_t)bv[j][e >> 2][e & 3];
-                    v = fmaf(__shfl(sum, 2 * e, 16), __uint_as_float(two << 16), v);
-                    v = fmaf(__shfl(sum, 2 * e + 1, 16), __uint_as_float(two & 0xFFFF0000u), v);
+                    sum_b = fmaf(__shfl(sum, 2 * e, 16), __uint_as_float(two << 16), sum_b);
+                    sum_b = fmaf(__shfl(sum, 2 * e + 1, 16), __uint_as_float(two & 0xFFFF0000u), sum_b);
                 }
             }
+            v += sum_b;
+        }
         if (o >= a.co) continue;
         const int m = m0 + row;
         if (a.out_f32) ((float*)a.y)[m * a.ldy + o] = v;

@@ -1064,3 +1064,22 @@ def test_group_norm_on_both_sides_of_every_form(torch, ee, dtype, pixels):
             ref, bound = norm_ref(torch, x, groups, None, None, 1e-5, "none", None, 5)
             got = ee.group_norm(x, groups, frac_bits=5)
             assert torch.equal(got, ref) if bound is None else bool(((got.double() - ref).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("rows,ci,co,r", [(12, 1, 16, 256), (64, 1, 76, 256), (400, 1, 65, 100), (1302, 1, 76, 256), (5000, 1, 9, 128), (33, 8, 100, 256)])
+def test_adapter_projection_small_adapters_beside_large_outputs(torch, ee, rows, ci, co, r):
+    """Many small terms of an adapter beside a bias a thousand times as large, whose float they are added to once: the bound has ci + 8 roundings of the large one, and those of the small ones among themselves."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g)
+    w, bias, ad = (rnd(co, ci) / ci ** 0.5).bfloat16(), 1000 * (1 + rnd(co).abs()), adapters_of(torch, g, 3, r, ci, co)
+    proj = ee.AdapterProjection(w, bias, adapters=3, rank=r)
+    for i, (a, b, s) in enumerate(ad):
+        proj.load(i, a, b, s)
+    for turn in range(8):
+        x = rnd(rows, ci).bfloat16()
+        ids = torch.randint(-1, 3, (rows,), device="cuda", generator=g, dtype=torch.int32)
+        say(f"[case] {rows} rows {ci} -> {co} rank {r}")
+        got = proj(x, ids, dtype=torch.float32)
+        ref, tol = project_ref(torch, x, w, bias, ad, ids, "fp32")
+        off = ((got.double() - ref).abs() / tol).cpu()
+        assert float(off.max()) <= 1, f"{float(off.max())} times the bound"
