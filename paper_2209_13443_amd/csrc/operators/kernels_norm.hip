@@ -204,7 +204,7 @@ __global__ __launch_bounds__(NT) void group_norm_kernel(NormKernelArgs a)
     if constexpr (FORM != 2) {
         // bf16: sums of x - pivot and of its square, the pivot first a value of the lane's own: as far from the mean as values of the group are.  mean and m2 hold them until 64 values (FORM 0: at most
         // 32) are added; these become a pair, which is merged with those before (`all`), and the next pivot is the mean up to there, rounded to bf16.  One sum over all values of a lane, up to
-        // 16,384 of them, lost what a first value far from the others left of the variance: 1024 x 1024 pixels of one value but for the first were 10 to 40 % off.
+        // 16,384 of them, lost what a first value far from the others left of the variance: 1024 x 1024 pixels of one value but for the first were 6 to 45 % off.
         // Vectors behind the lane's last pixel read as what adds nothing: pivots, int8 zeros
         stat_t st[GPV] = {}, all[ES == 2 && FORM == 1 ? GPV : 1] = {};
         float pivot[ES == 2 ? GPV : 1];
